@@ -16,7 +16,7 @@ import torch
 
 own = False
 DEV = "cuda"
-WORKSPACE_BYTES = 8 << 20
+WORKSPACE_BYTES = 16 << 20
 
 
 # ------------------------------------------------------------------------------------------------ cases
