@@ -52,6 +52,7 @@ extern "C" {
 #define FPT_ERR_WORKSPACE    -4   /* workspace missing or smaller than required         */
 #define FPT_ERR_CUDA         -5   /* a CUDA runtime / driver call failed                */
 #define FPT_ERR_TIMEOUT      -6   /* a device-side wait gave up (see fpt_check_status)  */
+#define FPT_ERR_INDEX        -7   /* a page, position or offset out of range was met on the device (fpt_check_status) */
 
 /* ---- enums -------------------------------------------------------------------- */
 #define FPT_DTYPE_BF16 0
@@ -79,6 +80,7 @@ extern "C" {
 #define FPT_OP_GEMM_A8   3     /* fpt_w4a8_gemm                                   */
 #define FPT_OP_LINEAR_A8 4     /* fpt_w4a4_linear / _dynamic with 8-bit activations */
 #define FPT_OP_MLP_HADAMARD 5  /* fpt_decoder_mlp with mid_hadamard = 1              */
+#define FPT_OP_ATTN 6          /* fpt_rope_append, fpt_kv_gather, fpt_attn_decode, fpt_attn_prompt */
 
 /* One quantiser, as the paper parametrises it: bit-width, grid kind, static scale and
  * offset (App. D "General set-up"). HOST struct. */
@@ -355,6 +357,99 @@ int fpt_decoder_attn_out(void* stream, const void* A, int M, int k_o,
                          void* Y, void* workspace, size_t workspace_bytes);
 
 /*
+ * The attention between the two calls above: rotary positions, a paged key/value cache in 8 bits (the KV8 of the
+ * W4A8KV8 setting, Sec. 4), attention of whole prompts and of single tokens.  The paper keeps this part in 16-bit
+ * floating point in its timing runs and prints no formulas for it; those below are this library's.
+ *
+ * Sequences are packed one behind the other: rows cu[s] .. cu[s+1]-1 of a buffer belong to sequence s, cu is a device
+ * array of n_seqs + 1 ascending int32 with cu[0] >= 0.  Rows outside (behind the last sequence of a padded batch) are
+ * neither read for a result nor written.  head_dim is 64 or 128, n_q a multiple of n_kv: query head h reads
+ * key/value head h / (n_q / n_kv).  Leading dimensions count elements and are multiples of 8; every pointer to 16-bit
+ * or 8-bit values is 16-byte aligned, every other one naturally.
+ *
+ * Lengths, offsets, positions and page numbers lie on the device and are not known to the host: one out of range
+ * never leads outside a buffer; it is recorded in the status word (fpt_check_status returns FPT_ERR_INDEX until
+ * fpt_reset_status), and the results of the sequences it concerns are unspecified.
+ *
+ * The four calls take a workspace of fpt_workspace_bytes(FPT_OP_ATTN, 1, 1, 1) bytes (any sizes), cleared once by
+ * fpt_reset_status.  It may be the one that the linears use if it is large enough, and as there, calls that may run
+ * at the same time need one each.
+ */
+
+/* Which elements of a head are turned together (i < rot_dim / 2): */
+#define FPT_ROPE_HALF        0    /* i and i + rot_dim / 2                              */
+#define FPT_ROPE_INTERLEAVED 1    /* 2 i and 2 i + 1                                    */
+
+/* A paged cache.  Token t of sequence s lies in slot t % page of page pages[s, t / page].  HOST struct, DEVICE pointers. */
+typedef struct fpt_kv_cache {
+  int8_t*        k;         /* [n_pages, n_kv, page, head_dim] codes, -127 .. 127                     */
+  int8_t*        v;
+  float*         k_scale;   /* [n_pages, n_kv]: value = code * scale                                  */
+  float*         v_scale;
+  const int32_t* pages;     /* [n_seqs, max_pages]                                                    */
+  int n_pages, n_kv, page, head_dim;      /* page: 16, 32, 64 or 128 tokens                           */
+  int max_pages;
+} fpt_kv_cache;
+
+/*
+ * Rotary positions of new tokens' queries and keys, and the append of keys and values to the cache.
+ *   QKV [M, ld] bf16 as fpt_decoder_attn_qkv leaves it: n_q | n_kv | n_kv heads of head_dim; rows packed by cu_new.
+ *   cu_new [n_seqs + 1] or NULL: row s is the one new token of sequence s (n_seqs <= M)
+ *   ctx [n_seqs] int32: tokens a sequence has before; token j of sequence s has position ctx[s] + j
+ *   rope [n_pos, rot_dim / 2, 2] f32: cos and sin of each position and pair (any base and scaling of the angles;
+ *        paper_2506_04985_b200/rope.py makes such tables); rot_dim % 16 == 0, rot_dim <= head_dim
+ *   rotation (float32, one rounding per operation, then one to bf16); elements from rot_dim on stay:
+ *        a' = a cos - b sin,  b' = b cos + a sin
+ *   Q_out [M, ld_q], n_q heads; K_out [M, ld_k], n_kv heads, or NULL.  Each may be its own place in QKV (same address
+ *        and leading dimension); otherwise they overlap nothing.
+ *   cache NULL or cache->k NULL: no append (n_kv and head_dim are then read from the struct all the same, so it is
+ *        required).  With it, for each page and head that gets new tokens:
+ *        m = max |v| over the new finite values, keys after their rounding to bf16
+ *        s = max(s_old, m / 127), s_old = 0 where the page held no earlier token of the sequence  (float32 division)
+ *        inv = 1 / s  (0 where s < 2^-126: such a page holds zeros)
+ *        new codes  clamp(rne(v * inv), -127, 127), infinities end at the clamp, a NaN gives -127
+ *        held codes clamp(rne(q * (s_old * inv)), -127, 127) where s > s_old
+ *     so a page's scale grows with its tokens and never shrinks while it keeps one (tokens taken back by a smaller ctx
+ *     keep their part in it).  A page that a call writes belongs to one sequence.
+ */
+int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int n_q,
+                    const float* rope, int n_pos, int rot_dim, int layout,
+                    const int32_t* cu_new, const int32_t* ctx, int n_seqs, const fpt_kv_cache* cache,
+                    void* Q_out, int ld_q, void* K_out, int ld_k, void* workspace, size_t workspace_bytes);
+
+/*
+ * Cached tokens in 16 bits: row cu_out[s] + i of K_out and V_out [M, ld] (n_kv heads of head_dim) becomes
+ * bf16(code * scale) of token first[s] + i (first NULL: 0).
+ */
+int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int32_t* first, const int32_t* cu_out, int n_seqs,
+                  int M, void* K_out, void* V_out, int ld, void* workspace, size_t workspace_bytes);
+
+/*
+ * Attention of one token a sequence over the cache:
+ *   z_t = scale * sum_d q_d k_td,  O = sum_t softmax(z)_t v_t,  lse = log sum_t exp(z_t),   t < kv_len[s]
+ *   Q [n_seqs, ld_q] bf16 and O [n_seqs, ld_o] bf16: n_q heads, O must not overlap Q; lse [n_seqs, n_q] f32 or NULL
+ *   kv_len [n_seqs] int32, the new token included; 0: O = 0, lse = -inf.
+ * A key or value is code * scale; pages whose value scale is below 2^-80 count as zeros.  The sums are float32; the weights
+ * enter the second product in fp16, scaled so that the largest is 2^14, queries the first one in fp16 after division by
+ * a power of two that brings the head's largest magnitude into [2^14, 2^15) (exact but for values below 2^-28 of that).  The long axis is split over the SMs by
+ * the lengths of all sequences: the same call gives the same bits, another batch may round a sequence's sums otherwise.
+ */
+int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, const fpt_kv_cache* cache, const int32_t* kv_len,
+                    int n_seqs, float scale, void* O, int ld_o, float* lse, void* workspace, size_t workspace_bytes);
+
+/*
+ * Attention of packed prompts: row i of sequence s (of len_q rows) sees keys j < len_k of the same sequence, with
+ * causal = 1 only those with j <= i + (len_k - len_q), so that the last query sees the last key; a row that sees none gives O = 0, lse = -inf.
+ *   Q [M_q, ld_q], K and V [M_k, ld_k], [M_k, ld_v], O [M_q, ld_o] bf16; lse [M_q, n_q] f32 or NULL
+ *   cu_q, cu_k [n_seqs + 1]; cu_k NULL: cu_q.  Q, K and V may be places in one buffer; O overlaps none of them.
+ * float32 scores and sums; the weights enter the second product in bf16.  Values of hidden keys, infinities and NaN
+ * among them, reach no result.
+ */
+int fpt_attn_prompt(void* stream, const void* Q, int ld_q, int M_q, const void* K, int ld_k, const void* V, int ld_v,
+                    int M_k, int n_q, int n_kv, int head_dim, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,
+                    int causal, float scale, void* O, int ld_o, float* lse, void* workspace, size_t workspace_bytes);
+
+/*
  * Measurement aid; the paper has no counterpart.  Runs nothing of the path: one thread per CTA
  * (pair = 0) or per pair of CTAs (pair = 1, `ctas` even) issues 4 * iters 8-bit integer
  * tensor-core instructions of 128 (pair: 256) rows x n columns x 32 codes on operand tiles that
@@ -383,7 +478,8 @@ int fpt_probe_mma(void* stream, int pair, int n, int n_acc, int a_in_tmem, int i
 int fpt_selftest_wait_timeout(void* stream, void* workspace, unsigned int limit_us, unsigned int* gave_up);
 
 /* Bytes of caller-provided scratch an entry point needs (op = FPT_OP_*).
- * FPT_OP_LINEAR / FPT_OP_GEMM / FPT_OP_GEMM_A8 / FPT_OP_LINEAR_A8: (M, N, K); FPT_OP_MLP: (M, d_ff, d). */
+ * FPT_OP_LINEAR / FPT_OP_GEMM / FPT_OP_GEMM_A8 / FPT_OP_LINEAR_A8: (M, N, K); FPT_OP_MLP: (M, d_ff, d);
+ * FPT_OP_ATTN: any sizes (one size serves all). */
 size_t fpt_workspace_bytes(int op, int M, int N, int K);
 
 /* Zeroes the control block (first 8 KiB: status word, tile counters) of a workspace.  Call once
@@ -392,7 +488,7 @@ int fpt_reset_status(void* stream, void* workspace);
 
 /* Synchronises `stream`, reads the status word at the start of `workspace` and returns
  * FPT_OK, FPT_ERR_TIMEOUT (a bounded device-side wait expired; the kernel released its
- * resources and returned, outputs are invalid) or FPT_ERR_CUDA. */
+ * resources and returned, outputs are invalid), FPT_ERR_INDEX (the attention calls) or FPT_ERR_CUDA. */
 int fpt_check_status(void* stream, void* workspace);
 
 #ifdef __cplusplus

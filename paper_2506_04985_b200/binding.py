@@ -14,18 +14,19 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfpt_b200.so")
 
 OK = 0
-ERR_BAD_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = -1, -2, -3, -4, -5, -6
+ERR_BAD_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = -1, -2, -3, -4, -5, -6, -7
 DTYPE_BF16, DTYPE_F32, DTYPE_F16 = 0, 1, 2
 RANGE_MINMAX, RANGE_LP = 0, 1
 RMSNORM, SCALE_INPUT, SILU_MUL, GU_INTERLEAVED = 1, 2, 4, 8
 POST_NONE, POST_INVERSE_OF_PRE, POST_VECTOR = 0, 1, 2
-OP_LINEAR, OP_MLP, OP_GEMM, OP_GEMM_A8, OP_LINEAR_A8, OP_MLP_HADAMARD = 0, 1, 2, 3, 4, 5
+OP_LINEAR, OP_MLP, OP_GEMM, OP_GEMM_A8, OP_LINEAR_A8, OP_MLP_HADAMARD, OP_ATTN = 0, 1, 2, 3, 4, 5, 6
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 
 EXPORTS = ["fpt_version", "fpt_strerror", "fpt_quantize_weights", "fpt_interleave_gate_up", "fpt_act_quant", "fpt_hadamard_quant",
            "fpt_w4a4_gemm", "fpt_w4a4_linear", "fpt_w4a4_linear_static", "fpt_decoder_mlp", "fpt_decoder_attn_qkv",
            "fpt_decoder_attn_out", "fpt_act_quant_dynamic", "fpt_w4a4_linear_dynamic", "fpt_w4a8_gemm", "fpt_workspace_bytes",
            "fpt_reset_status",
-           "fpt_check_status", "fpt_probe_mma", "fpt_set_programmatic_launch", "fpt_selftest_wait_timeout"]
+           "fpt_check_status", "fpt_rope_append", "fpt_kv_gather", "fpt_attn_decode", "fpt_attn_prompt", "fpt_probe_mma", "fpt_set_programmatic_launch", "fpt_selftest_wait_timeout"]
 
 
 class QParams(ctypes.Structure):
@@ -35,6 +36,40 @@ class QParams(ctypes.Structure):
 
     def __init__(self, bits=4, symmetric=True, scale=1.0, zero_point=0):
         super().__init__(int(bits), int(bool(symmetric)), float(scale), int(zero_point))
+
+
+class _KVCacheStruct(ctypes.Structure):
+    """Mirror of `fpt_kv_cache`."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "pages")] +
+                [(n, ctypes.c_int) for n in ("n_pages", "n_kv", "page", "head_dim", "max_pages")])
+
+
+class KVCache:
+    """A paged 8-bit cache (see `fpt_kv_cache`): codes int8 [n_pages, n_kv, page, head_dim], scales f32 [n_pages, n_kv],
+    page table int32 [n_seqs, max_pages], all contiguous on one device."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_kv", "head_dim", "struct", "ref")
+
+    def __init__(self, k, v, k_scale, v_scale, pages):
+        n_pages, n_kv, page, hd = k.shape
+        for t, dtype, shape in ((k, torch.int8, k.shape), (v, torch.int8, k.shape), (k_scale, torch.float32, (n_pages, n_kv)),
+                                (v_scale, torch.float32, (n_pages, n_kv)), (pages, torch.int32, pages.shape)):
+            if t.dtype is not dtype or t.shape != shape or t.dim() < 2 or not t.is_contiguous():
+                raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table are wanted")
+        self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
+        self.n_kv, self.head_dim = n_kv, hd
+        self.struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages.data_ptr(),
+                                     n_pages, n_kv, page, hd, pages.shape[1])
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def heads(cls, n_kv, head_dim):
+        """Stands for no storage: fpt_rope_append then only rotates."""
+        c = cls.__new__(cls)
+        c.k = c.v = c.k_scale = c.v_scale = c.pages = None
+        c.n_kv, c.head_dim = n_kv, head_dim
+        c.struct = _KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0)
+        c.ref = ctypes.byref(c.struct)
+        return c
 
 
 class FptError(RuntimeError):
@@ -85,6 +120,10 @@ def lib():
         L.fpt_w4a4_linear_dynamic.argtypes = [vp, vp, ci, ci, vp, vp, ci, ci, ci, ci, cf, vp, ci, vp, vp, vp, vp, sz]
         L.fpt_decoder_attn_qkv.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, ci, qp, cf, vp, vp, vp, vp, vp, sz]
         L.fpt_decoder_attn_out.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, ci, qp, vp, vp, vp, vp, vp, sz]
+        L.fpt_rope_append.argtypes = [vp, vp, ci, ci, ci, vp, ci, ci, ci, vp, vp, ci, vp, vp, ci, vp, ci, vp, sz]
+        L.fpt_kv_gather.argtypes = [vp, vp, vp, vp, ci, ci, vp, vp, ci, vp, sz]
+        L.fpt_attn_decode.argtypes = [vp, vp, ci, ci, vp, vp, ci, cf, vp, ci, vp, vp, sz]
+        L.fpt_attn_prompt.argtypes = [vp, vp, ci, ci, vp, ci, vp, ci, ci, ci, ci, ci, vp, vp, ci, ci, cf, vp, ci, vp, vp, sz]
         L.fpt_workspace_bytes.restype = sz
         L.fpt_workspace_bytes.argtypes = [ci, ci, ci, ci]
         L.fpt_reset_status.argtypes = [vp, vp]
@@ -301,6 +340,114 @@ def fpt_decoder_attn_out(A, Wo_q, sw_o, qp_ap, s_n, X=None, r=None, wsum=None, w
                                       d, ctypes.byref(qp_ap), _ptr(s_n), _ptr(X), _ptr(r), _ptr(Y), _ptr(ws),
                                       ws.numel()), "fpt_decoder_attn_out")
     return Y
+
+
+def new_kv_cache(n_pages, n_kv, page, head_dim, pages, device="cuda"):
+    """An empty cache around the page table `pages` (int32 [n_seqs, max_pages] on the device): codes and scales zero."""
+    k, v = (_empty((n_pages, n_kv, page, head_dim), dtype=torch.int8, device=device).zero_() for _ in range(2))
+    ks, vs = (_empty((n_pages, n_kv), dtype=torch.float32, device=device).zero_() for _ in range(2))
+    return KVCache(k, v, ks, vs, pages)
+
+
+# What the attention calls ask of a tensor (their rows may be places in a wider buffer).
+def _rows(t, where):
+    """Leading dimension of a bf16 [rows, columns] tensor whose rows are contiguous."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise FptError(ERR_BAD_ARG, where)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _i32(t, n, where):
+    """Address of an int32 [n] tensor."""
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise FptError(ERR_BAD_ARG, where)
+    return t.data_ptr()
+
+
+def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, want_k=False, Q=None, K=None, ws=None):
+    """QKV [M, (n_q + 2 n_kv) head_dim] bf16, rope f32 [n_pos, rot_dim / 2, 2], ctx int32 [n_seqs], cu_new int32 [n_seqs + 1]
+    (None: row s is sequence s's token) -> (rotated queries bf16 [M, n_q head_dim], rotated keys [M, n_kv head_dim] or None).
+    Keys and values go to the cache (KVCache.heads(n_kv, head_dim): nowhere)."""
+    M, cols = QKV.shape
+    ld, hd, n_kv = _rows(QKV, "fpt_rope_append"), cache.head_dim, cache.n_kv
+    if (rope.dtype is not torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or
+            cols < (n_q + 2 * n_kv) * hd or (cache.pages is not None and cache.pages.shape[0] < ctx.shape[0])):
+        raise FptError(ERR_BAD_ARG, "fpt_rope_append")
+    n = ctx.shape[0]
+    if Q is None:
+        Q = _empty((M, n_q * hd), dtype=torch.bfloat16, device=QKV.device)
+    if K is None and want_k:
+        K = _empty((M, n_kv * hd), dtype=torch.bfloat16, device=QKV.device)
+    if ws is None:
+        ws = new_workspace(OP_ATTN, 1, 1, 1, QKV.device)
+    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, ld, n_q, rope.data_ptr(), rope.shape[0], 2 * rope.shape[1], layout,
+                                 None if cu_new is None else _i32(cu_new, n + 1, "fpt_rope_append"),
+                                 _i32(ctx, n, "fpt_rope_append"), n, cache.ref, Q.data_ptr(), _rows(Q, "fpt_rope_append"),
+                                 _ptr(K), 0 if K is None else _rows(K, "fpt_rope_append"), ws.data_ptr(), ws.numel()),
+           "fpt_rope_append")
+    return Q, K
+
+
+def fpt_kv_gather(cache, cu_out, M, first=None, K=None, V=None, ws=None):
+    """Cached tokens first[s] ... of every sequence in bf16 -> (K, V) [M, n_kv head_dim], packed by cu_out int32 [n_seqs + 1]."""
+    n, cols = cu_out.shape[0] - 1, cache.n_kv * cache.head_dim
+    if cache.pages is None or cache.pages.shape[0] < n:
+        raise FptError(ERR_BAD_ARG, "fpt_kv_gather")
+    if K is None:
+        K = _empty((M, cols), dtype=torch.bfloat16, device=cu_out.device)
+    if V is None:
+        V = _empty((M, cols), dtype=torch.bfloat16, device=cu_out.device)
+    if ws is None:
+        ws = new_workspace(OP_ATTN, 1, 1, 1, cu_out.device)
+    ld = _rows(K, "fpt_kv_gather")
+    if _rows(V, "fpt_kv_gather") != ld or K.shape[0] < M or V.shape[0] < M:
+        raise FptError(ERR_BAD_ARG, "fpt_kv_gather")
+    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, "fpt_kv_gather"),
+                               _i32(cu_out, n + 1, "fpt_kv_gather"), n, M, K.data_ptr(), V.data_ptr(), ld, ws.data_ptr(), ws.numel()),
+           "fpt_kv_gather")
+    return K, V
+
+
+def fpt_attn_decode(Q, cache, kv_len, scale=None, want_lse=False, O=None, ws=None):
+    """Q [n_seqs, n_q head_dim] bf16, kv_len int32 [n_seqs] -> (O like Q, lse f32 [n_seqs, n_q] or None)."""
+    n, cols = Q.shape
+    hd = cache.head_dim
+    if cache.pages is None or cache.pages.shape[0] < n or cols % hd:
+        raise FptError(ERR_BAD_ARG, "fpt_attn_decode")
+    if O is None:
+        O = _empty((n, cols), dtype=torch.bfloat16, device=Q.device)
+    elif O.shape != Q.shape:
+        raise FptError(ERR_BAD_ARG, "fpt_attn_decode")
+    lse = _empty((n, cols // hd), dtype=torch.float32, device=Q.device) if want_lse else None
+    if ws is None:
+        ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
+    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, "fpt_attn_decode"), cols // hd, cache.ref,
+                                 _i32(kv_len, n, "fpt_attn_decode"), n, hd ** -0.5 if scale is None else scale, O.data_ptr(),
+                                 _rows(O, "fpt_attn_decode"), _ptr(lse), ws.data_ptr(), ws.numel()), "fpt_attn_decode")
+    return O, lse
+
+
+def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None, want_lse=False, O=None, ws=None):
+    """Q [M_q, n_q head_dim], K and V [M_k, n_kv head_dim] bf16 (places in wider buffers will do), packed by cu_q, cu_k int32
+    [n_seqs + 1] (cu_k None: cu_q) -> (O like Q, lse f32 [M_q, n_q] or None)."""
+    Mq, cols = Q.shape
+    hd, n = cols // n_q, cu_q.shape[0] - 1
+    if cols != n_q * hd or K.shape[1] != n_kv * hd or V.shape != K.shape:
+        raise FptError(ERR_BAD_ARG, "fpt_attn_prompt")
+    if O is None:
+        O = _empty((Mq, cols), dtype=torch.bfloat16, device=Q.device)
+    elif O.shape != Q.shape:
+        raise FptError(ERR_BAD_ARG, "fpt_attn_prompt")
+    lse = _empty((Mq, n_q), dtype=torch.float32, device=Q.device) if want_lse else None
+    if ws is None:
+        ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
+    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, "fpt_attn_prompt"), Mq, K.data_ptr(),
+                                 _rows(K, "fpt_attn_prompt"), V.data_ptr(), _rows(V, "fpt_attn_prompt"), K.shape[0], n_q, n_kv, hd,
+                                 _i32(cu_q, n + 1, "fpt_attn_prompt"),
+                                 None if cu_k is None else _i32(cu_k, n + 1, "fpt_attn_prompt"), n, int(bool(causal)),
+                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, "fpt_attn_prompt"), _ptr(lse),
+                                 ws.data_ptr(), ws.numel()), "fpt_attn_prompt")
+    return O, lse
 
 
 def fpt_act_quant_dynamic(X, bits=4, flags=RMSNORM, eps=1e-5, s_in=None, want_s_out=True, out=None):

@@ -1,6 +1,6 @@
 // C-ABI entry points that compose the kernels: argument checks, workspace carving,
 // launches.  No device memory is allocated here; everything lives in caller buffers.
-#include "fpt_internal.cuh"
+#include "attn_common.cuh"
 
 namespace fpt {
 
@@ -115,6 +115,7 @@ extern "C" const char* fpt_strerror(int code) {
     case FPT_ERR_WORKSPACE: return "workspace missing or too small";
     case FPT_ERR_CUDA: return "CUDA call failed";
     case FPT_ERR_TIMEOUT: return "a device-side wait gave up";
+    case FPT_ERR_INDEX: return "a page, position, length or offset out of range was met on the device";
     default: return "unknown error code";
   }
 }
@@ -137,6 +138,8 @@ extern "C" size_t fpt_workspace_bytes(int op, int M, int N, int K) {
       return kStatusBytes + gemm_scratch_bytes(M) + up256(m * d / 2) + 2 * up256(m * 4) +
              up256(mlp_gu_bytes(M, N, op == FPT_OP_MLP_HADAMARD)) + up256(m * dff / 2);
     }
+    case FPT_OP_ATTN:
+      return attn_workspace_bytes();
     default:
       return 0;
   }
@@ -153,7 +156,7 @@ extern "C" int fpt_check_status(void* stream, void* workspace) {
   if (cudaMemcpyAsync(&word, workspace, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess)
     return FPT_ERR_CUDA;
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return FPT_ERR_CUDA;
-  return word == 0 ? FPT_OK : FPT_ERR_TIMEOUT;
+  return word == 0 ? FPT_OK : (word & ~0xFFu) == kStatusIndexBase ? FPT_ERR_INDEX : FPT_ERR_TIMEOUT;
 }
 
 // fpt_w4a4_gemm; `early`: see GemmParams::early_weights, `wide`: the codes are widened, [M, K] bytes (only the composed

@@ -1,0 +1,68 @@
+// What the attention kernels share: 8-bit codes into floating point, the packed-sequence task search, the argument
+// checks of a paged cache.
+#pragma once
+
+#include "fpt_internal.cuh"
+
+namespace fpt {
+
+constexpr uint32_t kStatusIndexBase = 0x7200u;       // status word: a page, position, length or offset was out of range
+enum : uint32_t { kBadPage = 1, kBadPosition = 2, kBadLength = 3, kBadOffset = 4 };
+
+// First one wins; a time-out is never covered up.
+__device__ __forceinline__ void record_bad_index(uint32_t* status, uint32_t what) {
+  atomicCAS(status, 0u, kStatusIndexBase | what);
+}
+
+// The i-th of four two's complement bytes whose sign bits the caller has flipped, as a float32: 2^23 + (code + 128) is
+// one byte permutation, and the subtraction is exact.
+__device__ __forceinline__ float flipped_byte_to_f32(uint32_t flipped, int i) {
+  return __fsub_rn(__uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7440u | (uint32_t)i)), 8388736.0f);
+}
+
+// clamp(rne(x), -127, 127) in the low byte, a NaN -> -127 (fmaxf takes the other operand): after the clamp the sum with
+// 1.5 * 2^23 rounds to an integer, ties to even, whose two's complement low byte it carries.
+__device__ __forceinline__ uint32_t code_of(float x) {
+  return __float_as_uint(__fadd_rn(fminf(fmaxf(x, -127.0f), 127.0f), 12582912.0f));
+}
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d) {
+  return __byte_perm(__byte_perm(code_of(a), code_of(b), 0x0040u), __byte_perm(code_of(c), code_of(d), 0x0040u), 0x5410u);
+}
+
+// What a page's codes are multiplied with before rounding.
+__device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435e-38f ? __fdiv_rn(1.0f, s) : 0.0f; }
+
+// A launch over the pages (or blocks of `block` rows) that packed sequences touch, without their lengths on the host:
+// sequence s, rows cu[s] .. cu[s+1]-1, is given floor(cu[s+1] / block) - floor(cu[s] / block) + extra tasks, which
+// is at least the number of blocks of its rows (extra = 1: blocks count from its first row; 2: they count from any row), and
+// task `id` belongs to the last s whose tasks start at or before it.  All sequences are looked at side by side: one round of loads
+// where a binary search would wait for one load after the other.  Returns s or -1, the same in every thread, and the place among its tasks.
+__device__ __forceinline__ int find_task(const int32_t* __restrict__ cu, int n_seqs, int block, int extra, int id,
+                                         int* found /* shared, 2 ints */, uint32_t* status, int& place) {
+  if (threadIdx.x == 0) found[0] = -1;
+  __syncthreads();
+  for (int s = threadIdx.x; s < n_seqs; s += blockDim.x) {
+    const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1);
+    const int a = lo / block + extra * s, b = hi / block + extra * (s + 1);
+    if (lo < 0 || hi < lo) {
+      if (blockIdx.x == 0) record_bad_index(status, kBadOffset);
+    } else if (a <= id && id < b) {
+      found[0] = s;
+      found[1] = id - a;
+    }
+  }
+  __syncthreads();
+  place = found[1];
+  return found[0];
+}
+
+int check_cache(const fpt_kv_cache* c, bool with_storage);
+
+constexpr int kAttnMaxCtas = 640;         // launches of the single-token attention are never larger
+// A part of a row's result in the workspace: for at most 16 query heads the sums [head_dim], the reference exponent and the
+// sum of weights, float32.
+constexpr int kAttnPartFloats = 16 * (128 + 2);
+constexpr size_t kAttnScratchBytes = (size_t)kAttnMaxCtas * 2 * kAttnPartFloats * 4;
+inline size_t attn_workspace_bytes() { return kStatusBytes + kAttnScratchBytes; }
+
+}  // namespace fpt

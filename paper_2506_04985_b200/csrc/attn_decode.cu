@@ -1,0 +1,647 @@
+// Attention of one token a sequence over the paged 8-bit cache (fpt_attn_decode; formulas: include/fpt.h).
+//
+// Every cached code is read once and takes 2 * (query heads of the group) multiply-adds: the bound is the memory's rate.
+// So the kernel is a stream: a warp of each CTA requests tiles of 64 tokens (codes of keys and values) by TMA into a ring,
+// four warps take 16 tokens of a tile each.  The tiles of all sequences and key heads form one line that is cut into
+// equal ranges, one a CTA, whatever the lengths; a row (sequence, head) that is cut leaves partial results in the
+// workspace, and the CTA that finishes the row's last part joins them, in the order of the parts.
+//
+// A warp's arithmetic, per 16 tokens (T) and up to 8 NT query heads of the group (H):
+//   S^T[T x H] = K Q^T      m16n8k16, fp16 x fp16 -> fp32: codes are exact in fp16 (one byte permutation and one packed subtract make two), and
+//                           the elements' order along the sum is free: a thread's 16 contiguous codes are its operand registers
+//                           of four instructions, so keys need no transposition
+//   w = 2^(S' - M)          S' = S scale_k scale log2(e) + log2(scale_v), M the running maximum of S': the scale of the page's
+//                           values rides in the exponent, w is at most 2^14 (room below for the small ones in fp16)
+//   O^T[D x H] += V^T w     w through one 8x8 transposition between lanes; two tokens' bytes are interleaved by the
+//                           permutations that widen them, so values need no transposition either
+//   l += w / scale_v        float32, unrounded
+// Rows of the swizzled tile are taken in an order (token_row) in which eight lanes' 16-byte loads meet 32 different banks.
+#include "attn_common.cuh"
+
+namespace fpt {
+
+constexpr int kDecTile = 64;                       // tokens of a tile
+constexpr int kDecWarps = 4;                       // consumer warps, 16 tokens of a tile each
+constexpr int kDecThreads = (kDecWarps + 1) * 32;
+constexpr float kDecLift = 14.0f;                  // log2 of the largest weight
+constexpr float kDecTinyV = 8.271806125530277e-25f;    // 2^-80
+
+struct DecodeParams {
+  const __nv_bfloat16* Q;
+  const int32_t* kv_len;
+  const int32_t* pages;
+  const float *k_scale, *v_scale;
+  __nv_bfloat16* O;
+  float* lse;
+  uint32_t* ws;                 // control block: status word, counters
+  float* parts;                 // two a CTA, kAttnPartFloats each
+  int ld_q, ld_o, n_q, n_kv, group, blocks, n_seqs, n_pages, max_pages;   // blocks: of 8 NT query heads in a group
+  int page;
+  float scale_log2;             // scale * log2(e)
+};
+
+// One tile, as the producer leaves it for the consumers.
+struct __align__(16) TileInfo {
+  float ks[4];                  // per 16 tokens: scale of the keys * scale * log2(e)
+  float vl[4];                  // log2 of the scale of the values
+  int flags;                    // bit 0: first of this CTA's part of the row, 1: last of it, 2: the part is the whole row;
+                                // from bit 4: groups with values; from bit 8: tokens of the tile that count
+  int seq, head;                // head: kv head * blocks + block
+  uint32_t parts;               // of a part: CTA of the row's first part, and from bit 16 the number of parts
+};
+
+template <int HD, int NT, int ST>
+struct DecSmem {
+  static constexpr int kMat = kDecTile * HD;                     // bytes of a tile's keys (or values)
+  static constexpr int kQ = 8 * NT * HD * 2;
+  static constexpr int kRing = 0;
+  static constexpr int kQOff = ST * 2 * kMat;
+  static constexpr int kMergeOff = kQOff + ST * kQ;              // [warps][8 NT][HD] float
+  static constexpr int kMergeStats = kMergeOff + kDecWarps * 8 * NT * HD * 4;   // [warps][8 NT] {M, l}
+  static constexpr int kInfoOff = kMergeStats + kDecWarps * 8 * NT * 8;
+  static constexpr int kBarOff = kInfoOff + 64 * (int)sizeof(TileInfo);
+  static constexpr int kMiscOff = kBarOff + (2 * ST + 2) * 8;
+  static constexpr int kAlloc = kMiscOff + 16 + 1024;            // slack to align the base to 1024
+};
+
+// Row of the tile that stands at place l (0..15) of a 16-token group.
+__device__ __forceinline__ int token_row(int l) { return l ^ ((l & 1) << 2); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t half2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+
+// Two of the four sign-flipped bytes (code + 128) as fp16: 0x6400 + byte is 1024 + code + 128; the difference is exact.
+template <int SEL>
+__device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped) {
+  const uint32_t w = __byte_perm(flipped, 0x64646464u, SEL);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __floats2half2_rn(1152.0f, 1152.0f));
+  return half2_bits(h);
+}
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+
+// CTA of tile x where `total` tiles are cut into `ctas` ranges that start at floor(i * total / ctas).
+__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) { return (int)(((x + 1) * ctas - 1) / total); }
+
+__device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile : 1; }
+
+// Joins the parts of a row: thread `tid` of 128, heads [0, gh).  part(i): the i-th part's floats; out(head, d, value, M, l).
+template <int HD>
+struct PartView {
+  const float* p;
+  int width;                    // heads a part has room for
+  __device__ __forceinline__ const float* sums(int h) const { return p + (size_t)h * HD; }
+  __device__ __forceinline__ float top(int h) const { return __ldcg(p + (size_t)width * HD + h); }
+  __device__ __forceinline__ float total(int h) const { return __ldcg(p + (size_t)width * HD + width + h); }
+};
+
+template <int HD, int NT, int ST, int MINB>
+__global__ void __launch_bounds__(kDecThreads, MINB)
+attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodeParams P) {
+  using L = DecSmem<HD, NT, ST>;
+  constexpr int NH = 8 * NT;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_u32(smem);
+  auto full = [&](int s) { return sbase + L::kBarOff + 8u * s; };
+  auto empty = [&](int s) { return sbase + L::kBarOff + 8u * (ST + s); };
+  const uint32_t met = sbase + L::kBarOff + 8u * (2 * ST);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + L::kMiscOff);
+  int* last_flag = reinterpret_cast<int*>(smem + L::kMiscOff + 4);
+  int* n_tiles_s = reinterpret_cast<int*>(smem + L::kMiscOff + 8);
+  TileInfo* infos = reinterpret_cast<TileInfo*>(smem + L::kInfoOff);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kDecWarps); }
+    mbar_init(met, kDecWarps);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+
+  // Every warp of the producer's needs: the number of tiles and this CTA's range of them.
+  const int heads = P.n_kv * P.blocks;
+  const int cap = P.max_pages * P.page;
+  int64_t first = 0, end = 0, total = 0;
+  int ctas = 1;
+  if (warp == kDecWarps) {
+    int64_t mine = 0;
+    bool bad = false;
+    for (int s = lane; s < P.n_seqs; s += 32) {
+      const int len = __ldg(P.kv_len + s);
+      bad |= len < 0 || len > cap;
+      mine += tiles_of(min(len, cap));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (bad && blockIdx.x == 0) record_bad_index(P.ws, kBadLength);
+    total = mine * heads;
+    ctas = (int)min((int64_t)gridDim.x, total);
+    if ((int)blockIdx.x < ctas) {
+      first = (int64_t)blockIdx.x * total / ctas;
+      end = (int64_t)(blockIdx.x + 1) * total / ctas;
+    }
+    if (lane == 0) *n_tiles_s = (int)(end - first);
+  }
+  __syncthreads();
+
+  if (warp == kDecWarps) {
+    // ------------------------------------------------------------------ producer
+    // sequence of the first tile: 32 sequences at a time
+    int seq = 0;
+    int64_t off = 0;                                  // first tile of sequence `seq`
+    if (first < end) {
+      for (int s0 = 0;; s0 += 32) {
+        const int s = s0 + lane;
+        const int64_t t = s < P.n_seqs ? (int64_t)tiles_of(min(__ldg(P.kv_len + s), cap)) * heads : 0;
+        int64_t incl = t;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += v;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, off + incl > first);
+        if (hit) {
+          const int src = __ffs(hit) - 1;
+          off += __shfl_sync(0xffffffffu, incl - t, src);
+          seq = s0 + src;
+          break;
+        }
+        off += __shfl_sync(0xffffffffu, incl, 31);
+        if (s0 + 32 >= P.n_seqs) { first = end; break; }           // (not reached: the tiles add up to `total`)
+      }
+    }
+    const int pieces_max = P.page >= kDecTile ? 1 : kDecTile / P.page;    // pages of a tile
+    const int piece = min(P.page, kDecTile);                              // their tokens
+    // What a lane knows about its tile of the next batch of 32: pages and scales are asked for a batch ahead.
+    TileInfo ti;
+    int page_row[4], tok_n = 0;
+    auto look = [&](int64_t base) {
+      const int64_t x = base + lane;
+      tok_n = 0; ti.flags = 0;
+      if (x >= end) return;
+      int s = seq;
+      int64_t o = off;
+      int len = min(__ldg(P.kv_len + s), cap);
+      int nt = tiles_of(len);
+      while (x >= o + (int64_t)nt * heads) {          // (x < total: there is a next sequence)
+        o += (int64_t)nt * heads;
+        ++s;
+        len = min(__ldg(P.kv_len + s), cap);
+        nt = tiles_of(len);
+      }
+      const int64_t in = x - o;
+      const int h = (int)(in / nt), t = (int)(in - (int64_t)h * nt);
+      ti.seq = s; ti.head = h;
+      tok_n = max(0, min(kDecTile, len - t * kDecTile));
+      const bool whole = x - t >= first && x - t + nt <= end;
+      const bool a = t == 0 || x == first, z = t == nt - 1 || x == end - 1;
+      ti.flags = (a ? 1 : 0) | (z ? 2 : 0) | (whole ? 4 : 0) | (tok_n << 8);
+      ti.parts = 0;
+      if (z && !whole) {
+        const int c0 = cta_of(x - t, total, ctas), c1 = cta_of(x - t + nt - 1, total, ctas);
+        ti.parts = (uint32_t)c0 | (uint32_t)(c1 - c0 + 1) << 16;
+      }
+      const int kv_head = h / P.blocks;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        page_row[i] = -1;
+        if (i < pieces_max && i * piece < tok_n) {
+          const int tok = t * kDecTile + i * piece;
+          int pg = __ldg(P.pages + (size_t)s * P.max_pages + tok / P.page);
+          const bool ok = pg >= 0 && pg < P.n_pages;
+          if (!ok) { record_bad_index(P.ws, kBadPage); pg = 0; }
+          const int cell = pg * P.n_kv + kv_head;
+          page_row[i] = cell * P.page + tok % P.page;
+          ti.ks[i] = __ldg(P.k_scale + cell) * P.scale_log2;
+          ti.vl[i] = __ldg(P.v_scale + cell);
+        }
+      }
+    };
+    auto publish = [&](int64_t base) {                // the look-ups, laid out per 16 tokens
+      const int64_t x = base + lane;
+      if (x >= end) return;
+      TileInfo out = ti;
+      const int per = piece / 16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // (index of the piece of group i, kept out of local memory: per is 1, 2 or 4)
+        const float k = per == 4 ? ti.ks[0] : per == 2 ? (i < 2 ? ti.ks[0] : ti.ks[1]) : ti.ks[i];
+        const float v = per == 4 ? ti.vl[0] : per == 2 ? (i < 2 ? ti.vl[0] : ti.vl[1]) : ti.vl[i];
+        const bool used = i * 16 < tok_n;
+        const bool live = v >= kDecTinyV;
+        out.ks[i] = used ? k : 0.0f;
+        out.vl[i] = !used ? 0.0f : v != v ? v : live ? log2f(v) : -80.0f;
+        if (used && (live || v != v)) out.flags |= 16 << i;
+      }
+      infos[(int)(x - first) & 63] = out;
+    };
+    int st = 0; uint32_t ph = 0, armed = 0, armed_par = 0;
+    bool ok = true;
+    if (first < end) { look(first); publish(first); }
+    for (int64_t base = first; ok && base < end; base += 32) {
+      __syncwarp();
+      int rows[4] = {page_row[0], page_row[1], page_row[2], page_row[3]};
+      const int my_flags = ti.flags, my_seq = ti.seq, my_head = ti.head;
+      // where the next batch starts to look
+      const int last_lane = (int)min((int64_t)31, end - 1 - base);
+      {
+        const int s_last = __shfl_sync(0xffffffffu, my_seq, last_lane);
+        while (seq < s_last) { off += (int64_t)tiles_of(min(__ldg(P.kv_len + seq), cap)) * heads; ++seq; }
+      }
+      if (base + 32 < end) look(base + 32);
+      const int count = last_lane + 1;
+      for (int i = 0; i < count; ++i) {
+        const int fl = __shfl_sync(0xffffffffu, my_flags, i);
+        const int sq = __shfl_sync(0xffffffffu, my_seq, i), hd = __shfl_sync(0xffffffffu, my_head, i);
+        int r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = __shfl_sync(0xffffffffu, rows[j], i);
+        if (!mbar_wait_warp(empty(st), ph ^ 1u, abort_flag, P.ws, 1)) { ok = false; break; }
+        if (lane == 0) {
+          int boxes = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) boxes += r[j] >= 0;
+          const int kvh = hd / P.blocks, blk = hd - kvh * P.blocks;
+          const int gh = min(NH, P.group - blk * NH);
+          const uint32_t qb = (fl & 1) ? (uint32_t)gh * HD * 2 : 0u;
+          mbar_arrive_expect_tx(full(st), (uint32_t)boxes * piece * HD * 2 + qb);
+          const uint32_t dst = sbase + L::kRing + st * 2 * L::kMat;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (r[j] >= 0) {
+              tma_load_2d(dst + j * piece * HD, &tmK, full(st), 0, r[j]);
+              tma_load_2d(dst + L::kMat + j * piece * HD, &tmV, full(st), 0, r[j]);
+            }
+          if (qb)
+            bulk_load_1d(sbase + L::kQOff + st * L::kQ,
+                         P.Q + (size_t)sq * P.ld_q + (size_t)(kvh * P.group + blk * NH) * HD, qb, full(st));
+        }
+        armed |= 1u << st;
+        armed_par = (armed_par & ~(1u << st)) | (ph << st);
+        if (++st == ST) { st = 0; ph ^= 1u; }
+      }
+      // The half of the ring that the next batch takes was read when the tile 32 back was let go, long before the last of
+      // these 32 could be requested (the ring of tiles is shorter).
+      if (ok && base + 32 < end) publish(base + 32);
+    }
+    if (!ok && lane == 0) {
+      const uint64_t t0 = globaltimer_ns();
+      for (int q = 0; q < ST; ++q)
+        if (armed & (1u << q))
+          while (!mbar_try_wait(full(q), (armed_par >> q) & 1u) && globaltimer_ns() - t0 < 2000000ull) {}
+    }
+  } else {
+    // ------------------------------------------------------------------ consumers
+    constexpr int KS = HD / 16;                       // k-steps of S, and 16-row tiles of O
+    const int g = lane >> 2, q = lane & 3;
+    const int n_tiles = *n_tiles_s;
+    const int row_a = warp * 16 + token_row(g), row_b = row_a + 8;            // keys: this lane's two rows
+    const int tok0 = warp * 16 + token_row(2 * q), tok1 = warp * 16 + token_row(2 * q + 1);
+    auto chunk = [&](int row, int c) -> int {                                   // byte of a row's 16-byte chunk
+      return HD == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+    };
+    float* merge = reinterpret_cast<float*>(smem + L::kMergeOff);
+    float2* stats = reinterpret_cast<float2*>(smem + L::kMergeStats);
+    uint32_t qf[NT][KS][2];
+    float qscale[NT][2];                              // of heads 2 q and 2 q + 1
+    float O[NT][KS][4];
+    float M[NT][2], l[NT][2];
+    int st = 0; uint32_t ph = 0, met_ph = 0;
+    // The consumer warps meet (a bounded wait: a named barrier would hold them for good where one of them has given up).
+    auto meet = [&]() -> bool {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(met);
+      const bool ok = mbar_wait_warp(met, met_ph, abort_flag, P.ws, 3);
+      met_ph ^= 1u;
+      return ok;
+    };
+    for (int i = 0; i < n_tiles; ++i) {
+      if (!mbar_wait_warp(full(st), ph, abort_flag, P.ws, 2)) break;
+      const TileInfo& ti = infos[i & 63];
+      const int flags = ti.flags, n = flags >> 8, head = ti.head;
+      if (flags & 1) {
+        const int blk = head % P.blocks;
+        const int gh = min(NH, P.group - blk * NH);
+        const uint8_t* qs = smem + L::kQOff + st * L::kQ;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          // this lane's 8 KS/2 ... elements of head 8 t + g: of chunk c (16 elements), those of its quad place
+          uint32_t raw[KS][2];
+          uint32_t mag = 0;
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c) {
+            uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+            if (8 * t + g < gh) {
+              const uint4* src = reinterpret_cast<const uint4*>(qs + ((8 * t + g) * HD + (c * 4 + q) * 16) * 2);
+              lo = src[0]; hi = src[1];
+            }
+            raw[c * 4 + 0][0] = lo.x; raw[c * 4 + 0][1] = lo.y;
+            raw[c * 4 + 1][0] = lo.z; raw[c * 4 + 1][1] = lo.w;
+            raw[c * 4 + 2][0] = hi.x; raw[c * 4 + 2][1] = hi.y;
+            raw[c * 4 + 3][0] = hi.z; raw[c * 4 + 3][1] = hi.w;
+          }
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            mag = __vmaxu2(mag, raw[k][0] & 0x7FFF7FFFu);
+            mag = __vmaxu2(mag, raw[k][1] & 0x7FFF7FFFu);
+          }
+          mag = max(mag & 0xFFFFu, mag >> 16);
+          mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, 1));
+          mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, 2));
+          // 2^(14 - e) for a largest magnitude in [2^e, 2^(e+1)); two factors, since one may leave the range
+          int e = (int)(mag >> 7) - 127;
+          e = min(max(e, -126), 128);                 // (subnormal or zero: -126; not finite: 128, and the values stay so)
+          const float f1 = __uint_as_float((uint32_t)(127 + (14 - e) / 2) << 23);
+          const float f2 = __uint_as_float((uint32_t)(127 + (14 - e) - (14 - e) / 2) << 23);
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              qf[t][k][j] = half2_bits(__floats2half2_rn(bf16lo_to_f32(raw[k][j]) * f1 * f2, bf16hi_to_f32(raw[k][j]) * f1 * f2));
+          const float back = __uint_as_float((uint32_t)max(1, 127 + e - 14) << 23);      // 2^(e - 14)
+          qscale[t][0] = __shfl_sync(0xffffffffu, back, 8 * q);
+          qscale[t][1] = __shfl_sync(0xffffffffu, back, 8 * q + 4);
+          M[t][0] = M[t][1] = -INFINITY;
+          l[t][0] = l[t][1] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) O[t][k][0] = O[t][k][1] = O[t][k][2] = O[t][k][3] = 0.0f;
+        }
+      }
+      if (warp * 16 < n) {
+        const uint8_t* ks = smem + L::kRing + st * 2 * L::kMat;
+        const uint8_t* vs = ks + L::kMat;
+        const float kf = ti.ks[warp], vl = ti.vl[warp];
+        const bool v_live = (flags >> (4 + warp)) & 1;
+        float S[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = S[t][2] = S[t][3] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c) {
+          const uint4 ra = *reinterpret_cast<const uint4*>(ks + chunk(row_a, c * 4 + q));
+          const uint4 rb = *reinterpret_cast<const uint4*>(ks + chunk(row_b, c * 4 + q));
+          const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t fa = wa[w] ^ 0x80808080u, fb = wb[w] ^ 0x80808080u;
+            const uint32_t a0 = bytes_to_half2<0x4140>(fa), a2 = bytes_to_half2<0x4342>(fa);
+            const uint32_t a1 = bytes_to_half2<0x4140>(fb), a3 = bytes_to_half2<0x4342>(fb);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma_f16(S[t], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
+          }
+        }
+        uint32_t p0[NT], p1[NT];
+        const bool in_a = row_a < n, in_b = row_b < n;
+        const float inv_v = ex2(-vl);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float f0 = qscale[t][0] * kf, f1 = qscale[t][1] * kf;
+          float s[4] = {fmaf(S[t][0], f0, vl), fmaf(S[t][1], f1, vl), fmaf(S[t][2], f0, vl), fmaf(S[t][3], f1, vl)};
+          if (!in_a) s[0] = s[1] = -INFINITY;
+          if (!in_b) s[2] = s[3] = -INFINITY;
+          float m0 = fmaxf(s[0], s[2]), m1 = fmaxf(s[1], s[3]);
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1) {
+            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+          }
+          if (__any_sync(0xffffffffu, m0 > M[t][0] || m1 > M[t][1])) {
+            const float n0 = fmaxf(M[t][0], m0), n1 = fmaxf(M[t][1], m1);
+            const float r0 = M[t][0] == -INFINITY ? 0.0f : ex2(M[t][0] - n0);
+            const float r1 = M[t][1] == -INFINITY ? 0.0f : ex2(M[t][1] - n1);
+            M[t][0] = n0; M[t][1] = n1;
+            l[t][0] *= r0; l[t][1] *= r1;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) { O[t][k][0] *= r0; O[t][k][1] *= r1; O[t][k][2] *= r0; O[t][k][3] *= r1; }
+          }
+          // a maximum of -inf: nothing counts yet, and no difference of infinities is formed
+          const float b0 = M[t][0] == -INFINITY ? 0.0f : M[t][0] - kDecLift, b1 = M[t][1] == -INFINITY ? 0.0f : M[t][1] - kDecLift;
+          float w[4] = {ex2(s[0] - b0), ex2(s[1] - b1), ex2(s[2] - b0), ex2(s[3] - b1)};
+          l[t][0] = fmaf(w[0] + w[2], inv_v, l[t][0]);
+          l[t][1] = fmaf(w[1] + w[3], inv_v, l[t][1]);
+          if (!v_live) w[0] = w[1] = w[2] = w[3] = 0.0f;
+          p0[t] = transpose8x8(half2_bits(__floats2half2_rn(w[0], w[1])));
+          p1[t] = transpose8x8(half2_bits(__floats2half2_rn(w[2], w[3])));
+        }
+        // values: tokens 2q, 2q+1, 2q+8, 2q+9 of the group, elements g * HD/8 ...
+        constexpr int W = HD / 32;
+        uint32_t v[4][W];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int row = (j & 1 ? tok1 : tok0) + (j >> 1) * 8;
+          if (HD == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(vs + chunk(row, g));
+            v[j][0] = x.x; v[j][1] = x.y; v[j][W - 2] = x.z; v[j][W - 1] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(vs + chunk(row, g >> 1) + (g & 1) * 8);
+            v[j][0] = x.x; v[j][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const uint32_t x0 = v[0][w] ^ 0x80808080u, x1 = v[1][w] ^ 0x80808080u;
+          const uint32_t x2 = v[2][w] ^ 0x80808080u, x3 = v[3][w] ^ 0x80808080u;
+          const uint32_t lo01 = __byte_perm(x0, x1, 0x5140), hi01 = __byte_perm(x0, x1, 0x7362);
+          const uint32_t lo23 = __byte_perm(x2, x3, 0x5140), hi23 = __byte_perm(x2, x3, 0x7362);
+          const uint32_t a0 = bytes_to_half2<0x4140>(lo01), a1 = bytes_to_half2<0x4342>(lo01);
+          const uint32_t a2 = bytes_to_half2<0x4140>(lo23), a3 = bytes_to_half2<0x4342>(lo23);
+          const uint32_t c0 = bytes_to_half2<0x4140>(hi01), c1 = bytes_to_half2<0x4342>(hi01);
+          const uint32_t c2 = bytes_to_half2<0x4140>(hi23), c3 = bytes_to_half2<0x4342>(hi23);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            mma_f16(O[t][2 * w], a0, a1, a2, a3, p0[t], p1[t]);
+            mma_f16(O[t][2 * w + 1], c0, c1, c2, c3, p0[t], p1[t]);
+          }
+        }
+      }
+      const int row_seq = ti.seq;                     // (before the tile is let go)
+      const int part0 = (int)(ti.parts & 0xFFFFu), nparts = (int)(ti.parts >> 16);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(st));
+      if (++st == ST) { st = 0; ph ^= 1u; }
+
+      if (flags & 2) {
+        // ---------------------------------------------------------------- end of this CTA's part of a row
+        const int kvh = head / P.blocks, blk = head - kvh * P.blocks;
+        const int gh = min(NH, P.group - blk * NH);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1) {
+            l[t][0] += __shfl_xor_sync(0xffffffffu, l[t][0], o);
+            l[t][1] += __shfl_xor_sync(0xffffffffu, l[t][1], o);
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int h = 8 * t + 2 * q + j;
+            if (h < gh) {
+              if (g == 0) stats[warp * NH + h] = make_float2(M[t][j], l[t][j]);
+              float* dst = merge + (size_t)(warp * NH + h) * HD + g * (HD / 8);
+#pragma unroll
+              for (int k = 0; k < KS; ++k) { dst[2 * k] = O[t][k][j]; dst[2 * k + 1] = O[t][k][2 + j]; }
+            }
+          }
+        }
+        if (!meet()) break;
+        const int tid = threadIdx.x;
+        const size_t q0 = (size_t)kvh * P.group + (size_t)blk * NH;        // first query head of the row
+        auto emit = [&](int h, int d, float4 o, float m, float sum) {      // four elements of a finished head
+          const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+          uint2 w = make_uint2(f32x2_to_bf16x2_bits(o.x * inv, o.y * inv), f32x2_to_bf16x2_bits(o.z * inv, o.w * inv));
+          *reinterpret_cast<uint2*>(P.O + (size_t)row_seq * P.ld_o + (q0 + h) * HD + d) = w;
+          if (d == 0 && P.lse)
+            P.lse[(size_t)row_seq * P.n_q + q0 + h] =
+                sum > 0.0f || sum != sum ? (m - kDecLift) * 0.69314718055994531f + logf(sum) : -INFINITY;
+        };
+        constexpr int D4 = HD / 4;
+        float* part = P.parts + (size_t)(2 * (int)blockIdx.x + ((int)blockIdx.x == part0 ? 1 : 0)) * kAttnPartFloats;
+        for (int e = tid; e < gh * D4; e += kDecWarps * 32) {
+          const int h = e / D4, d = (e % D4) * 4;
+          float top = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < kDecWarps; ++w) top = fmaxf(top, stats[w * NH + h].x);
+          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          float sum = 0.0f;
+#pragma unroll
+          for (int w = 0; w < kDecWarps; ++w) {
+            const float2 ml = stats[w * NH + h];
+            const float r = ml.x == -INFINITY ? 0.0f : ex2(ml.x - top);
+            const float4 x = *reinterpret_cast<const float4*>(merge + (size_t)(w * NH + h) * HD + d);
+            o.x = fmaf(x.x, r, o.x); o.y = fmaf(x.y, r, o.y); o.z = fmaf(x.z, r, o.z); o.w = fmaf(x.w, r, o.w);
+            sum = fmaf(ml.y, r, sum);
+          }
+          if (flags & 4) {
+            emit(h, d, o, top, sum);
+          } else {
+            __stcg(reinterpret_cast<float4*>(part + (size_t)h * HD + d), o);
+            if (d == 0) { __stcg(part + NH * HD + h, top); __stcg(part + NH * HD + NH + h, sum); }
+          }
+        }
+        if (!(flags & 4)) {
+          __threadfence();
+          if (!meet()) break;
+          if (tid == 0) {
+            uint32_t* counter = P.ws + kCounterWord0 + part0;
+            const bool last = atomicAdd(counter, 1u) == (uint32_t)nparts - 1u;
+            if (last) *counter = 0;                   // as the next call finds it
+            __threadfence();
+            *last_flag = last;
+          }
+          if (!meet()) break;
+          if (*last_flag) {
+            // the row's parts, in their order: the first is the tail part of its CTA, the others head parts of theirs
+            auto view = [&](int p) {
+              return PartView<HD>{P.parts + (size_t)(2 * (part0 + p) + (p == 0 ? 1 : 0)) * kAttnPartFloats, NH};
+            };
+            for (int e = tid; e < gh * D4; e += kDecWarps * 32) {
+              const int h = e / D4, d = (e % D4) * 4;
+              float top = -INFINITY;
+              for (int p = 0; p < nparts; ++p) top = fmaxf(top, view(p).top(h));
+              float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              float sum = 0.0f;
+#pragma unroll 4
+              for (int p = 0; p < nparts; ++p) {
+                const PartView<HD> w = view(p);
+                const float m = w.top(h);
+                const float r = m == -INFINITY ? 0.0f : ex2(m - top);
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(w.sums(h) + d));
+                o.x = fmaf(x.x, r, o.x); o.y = fmaf(x.y, r, o.y); o.z = fmaf(x.z, r, o.z); o.w = fmaf(x.w, r, o.w);
+                sum = fmaf(w.total(h), r, sum);
+              }
+              emit(h, d, o, top, sum);
+            }
+          }
+        }
+        if (!meet()) break;                           // the buffers are free for the next row
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ host side
+static bool make_code_map(CUtensorMap* m, const void* base, int64_t rows, int hd, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)hd, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)hd};
+  const cuuint32_t box[2] = {(cuuint32_t)hd, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD, int NT, int ST, int MINB>
+static int launch_decode(cudaStream_t st, const fpt_kv_cache* c, DecodeParams P) {
+  using L = DecSmem<HD, NT, ST>;
+  static_assert((L::kAlloc + 1024) * MINB <= 228 * 1024, "the ring does not fit");
+  static_assert(ST < 32, "a batch of tiles has to be longer than the ring");
+  auto kern = attn_decode_kernel<HD, NT, ST, MINB>;
+  static PerDeviceInt attr_set;
+  if (!ensure_smem_attr(attr_set, kern, L::kAlloc)) return FPT_ERR_CUDA;
+  CUtensorMap tmK, tmV;
+  const int64_t rows = (int64_t)c->n_pages * c->n_kv * c->page;
+  const int box = c->page < kDecTile ? c->page : kDecTile;
+  if (!make_code_map(&tmK, c->k, rows, HD, box) || !make_code_map(&tmV, c->v, rows, HD, box)) return FPT_ERR_CUDA;
+  P.blocks = (P.group + 8 * NT - 1) / (8 * NT);
+  // a CTA for each tile at most
+  const int64_t most = (int64_t)P.n_seqs * P.n_kv * P.blocks * (((int64_t)c->max_pages * c->page + kDecTile - 1) / kDecTile);
+  int64_t grid = (int64_t)device_sm_count() * MINB;
+  if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
+  if (grid > most) grid = most;
+  return launch_kernel(kern, dim3((unsigned)grid), dim3(kDecThreads), L::kAlloc, st, true, tmK, tmV, P) == cudaSuccess
+             ? FPT_OK
+             : FPT_ERR_CUDA;
+}
+
+}  // namespace fpt
+
+using namespace fpt;
+
+extern "C" int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, const fpt_kv_cache* cache,
+                               const int32_t* kv_len, int n_seqs, float scale, void* O, int ld_o, float* lse,
+                               void* workspace, size_t workspace_bytes) {
+  if (!Q || !kv_len || !O || n_q <= 0 || n_seqs <= 0) return FPT_ERR_BAD_ARG;
+  const int rc = check_cache(cache, true);
+  if (rc) return rc;
+  if (n_q % cache->n_kv) return FPT_ERR_UNSUPPORTED;
+  if (ld_q < (int64_t)n_q * cache->head_dim || ld_o < (int64_t)n_q * cache->head_dim) return FPT_ERR_BAD_ARG;
+  if (!(scale > 0.0f) || !(scale < 1e30f)) return FPT_ERR_BAD_ARG;
+  if (ld_q % 8 || ld_o % 8 || (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)workspace) & 15)) return FPT_ERR_ALIGNMENT;
+  if (((uintptr_t)kv_len | (uintptr_t)lse) & 3) return FPT_ERR_ALIGNMENT;
+  if (!workspace || workspace_bytes < attn_workspace_bytes()) return FPT_ERR_WORKSPACE;
+  DecodeParams P{};
+  P.Q = reinterpret_cast<const __nv_bfloat16*>(Q);
+  P.kv_len = kv_len; P.pages = cache->pages; P.k_scale = cache->k_scale; P.v_scale = cache->v_scale;
+  P.O = reinterpret_cast<__nv_bfloat16*>(O);
+  P.lse = lse;
+  P.ws = reinterpret_cast<uint32_t*>(workspace);
+  P.parts = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kStatusBytes);
+  P.ld_q = ld_q; P.ld_o = ld_o; P.n_q = n_q; P.n_kv = cache->n_kv; P.group = n_q / cache->n_kv; P.n_seqs = n_seqs;
+  P.n_pages = cache->n_pages; P.max_pages = cache->max_pages; P.page = cache->page;
+  P.scale_log2 = scale * 1.4426950408889634f;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (cache->head_dim == 128)
+    return P.group <= 8 ? launch_decode<128, 1, 3, 3>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
+  return P.group <= 8 ? launch_decode<64, 1, 6, 3>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);
+}

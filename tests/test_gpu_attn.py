@@ -1,0 +1,468 @@
+"""Rotary positions with the append to the paged 8-bit cache, reading it back, attention over it and of whole prompts,
+against the oracle's float64 (and, where a rounding is defined, bit for bit)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as OA
+from paper_2506_04985_b200 import binding as B
+from helpers import DEV, bf16_host, guarded_empty, host
+
+pytestmark = pytest.mark.gpu
+
+HALF = 2.0 ** -8           # half a step of bf16, relative
+
+
+def bf16(rng, *shape, gain=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * gain).astype(np.float32)).to(torch.bfloat16)
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def offsets(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+
+
+def table(n_pos, rot, base=500000.0):
+    f = base ** (-np.arange(0, rot, 2) / rot)
+    a = np.arange(n_pos)[:, None] * f
+    return np.stack([np.cos(a), np.sin(a)], -1).astype(np.float32)
+
+
+def paged(rng, lens, page, n_kv, hd, spare=2, filled=True, width=0):
+    """A cache with the pages of the sequences in a random order: (KVCache, page table, codes and scales on the host)."""
+    need = [max(1, -(-n // page)) for n in lens]
+    n_pages = sum(need) + spare
+    order = rng.permutation(n_pages)
+    pages = np.full((len(lens), max(max(need), width)), -7, np.int32)      # what no length reaches is not looked at
+    at = 0
+    for i, n in enumerate(need):
+        pages[i, :n] = order[at:at + n]
+        at += n
+    shape = (n_pages, n_kv, page, hd)
+    codes = [rng.integers(-127, 128, shape).astype(np.int8) if filled else np.zeros(shape, np.int8) for _ in "kv"]
+    scales = [(rng.uniform(0.5, 4.0, shape[:2]) / 127).astype(np.float32) if filled else np.zeros(shape[:2], np.float32) for _ in "kv"]
+    dev = []
+    for a in (*codes, *scales):
+        t = guarded_empty(a.shape, torch.int8 if a.dtype == np.int8 else torch.float32)
+        t.copy_(torch.from_numpy(a))
+        dev.append(t)
+    return B.KVCache(*dev, i32(pages.tolist())), pages, codes, scales
+
+
+def workspace():
+    return B.new_workspace(B.OP_ATTN, 1, 1, 1)
+
+
+def close(got, want, bound, what):
+    """|got - want| <= bound, infinities and NaN in the same places."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    fine = np.isfinite(want)
+    assert (np.isfinite(got) == fine).all(), f"{what}: finite in other places"
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+    off = np.abs(got - want)[fine] - np.broadcast_to(bound, want.shape)[fine]
+    assert off.size == 0 or off.max() <= 0, f"{what}: {int((off > 0).sum())} of {off.size} off, worst by {off.max():.3g}"
+
+
+# Bounds of an attention output.  The result's rounding: HALF of it.  A weight's rounding (bf16: HALF, fp16: 2^-11) moves the
+# result by at most that share of the weighted mean of |v|.  An exponent is off by the float32 sums' error, at most
+# hd * 2^-24 * sum |q k| scale (sums of hd terms in any order; `mass` is the largest such sum), and by a few 2^-24 of itself and of the maximum
+# (|z| <= mass); times 1.45 for the change to base 2; the polynomial for powers is 2.7e-6 off, the instruction 2^-22.  A
+# weight e^x is off by the same share; numerator and denominator: twice.
+def out_bound(o, spread, mass, hd, weight_rounding):
+    share = 2 * (1.45 * (hd + 16) * 2.0 ** -24 * mass[..., None] + 3e-6 + 2.0 ** -20)
+    return HALF * np.abs(o) + (weight_rounding + share) * (1 + HALF) * spread + 1e-30
+
+
+def lse_bound(lse, mass, hd):
+    return 1.45 * (hd + 16) * 2.0 ** -24 * mass + 4e-6 + 2.0 ** -20 + 2.0 ** -21 * np.abs(np.where(np.isfinite(lse), lse, 0))
+
+
+# ------------------------------------------------------------------------------------------------ append
+APPEND = [
+    # hd, page, n_q, n_kv, rot, interleaved, new, ctx
+    (128, 64, 32, 8, 128, 0, [1] * 5, [0, 63, 64, 100, 1000]),
+    (128, 64, 8, 2, 64, 1, [70, 1, 0, 129, 64], [0, 5, 17, 63, 64]),
+    (128, 16, 4, 4, 32, 0, [33, 16, 1, 15], [1, 0, 15, 16]),
+    (128, 128, 7, 1, 128, 1, [300, 5], [130, 127]),
+    (128, 32, 10, 2, 16, 0, [31, 0, 0, 65], [0, 0, 7, 40]),
+    (64, 64, 12, 12, 64, 0, [65, 3, 200], [0, 62, 1]),
+    (64, 16, 16, 1, 64, 1, [1, 17, 40], [15, 16, 3]),
+    (64, 32, 6, 2, 48, 1, [50, 1], [20, 31]),
+    (64, 128, 2, 2, 32, 0, [129, 127, 300], [127, 1, 64]),
+]
+
+
+@pytest.mark.parametrize("hd,page,n_q,n_kv,rot,inter,new,ctx", APPEND)
+@pytest.mark.parametrize("odd", [False, True], ids=["plain", "odd values"])
+def test_append_matches_the_oracle_bit_for_bit(hd, page, n_q, n_kv, rot, inter, new, ctx, odd):
+    rng = np.random.default_rng(hd + page + rot + sum(new) + odd)
+    single = all(n == 1 for n in new)
+    rows, pad = sum(new), 3
+    heads = n_q + 2 * n_kv
+    ld = heads * hd + 24
+    buf = bf16(rng, rows + pad, ld)
+    if odd:
+        x = buf[:rows, :heads * hd].view(rows, heads, hd)
+        x[rows // 2, n_q:, 5] = math.inf
+        x[0, n_q:, hd - 1] = -math.inf
+        x[rows - 1, n_q:, rot // 2] = math.nan
+        x[:, n_q + n_kv] = 0                             # a value head of zeros
+        x[0, n_q + n_kv, 3] = 1e-38                       # ... but for one whose page's scale is below 2^-126
+    cache, pages, codes, scales = paged(rng, [c + n for c, n in zip(ctx, new)], page, n_kv, hd)
+    if odd:
+        for s in scales:
+            s[:, 0] = 0                                  # pages that hold zeros so far
+        cache.k_scale.copy_(torch.from_numpy(scales[0])), cache.v_scale.copy_(torch.from_numpy(scales[1]))
+    tab = table(max(c + n for c, n in zip(ctx, new)), rot)
+    qkv = buf.to(DEV)[:, :heads * hd]
+    Q = guarded_empty((rows + pad, n_q * hd), torch.bfloat16)
+    K = guarded_empty((rows + pad, n_kv * hd), torch.bfloat16)
+    Q.fill_(7.0), K.fill_(7.0)
+    ws = workspace()
+    cu = offsets(new)
+    B.fpt_rope_append(qkv, n_q, cache, torch.from_numpy(tab).to(DEV), i32(ctx), cu_new=None if single else i32(cu.tolist()),
+                      layout=B.ROPE_INTERLEAVED if inter else B.ROPE_HALF, Q=Q, K=K, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    x = buf[:, :heads * hd].float().numpy().reshape(rows + pad, heads, hd)
+    for i, (n, c) in enumerate(zip(new, ctx)):
+        a = cu[i]
+        with np.errstate(invalid="ignore"):
+            qk = OA.rope(x[a:a + n, :n_q + n_kv], tab[c:c + n], rot, inter)
+        assert np.array_equal(bf16_host(Q)[a:a + n], qk[:, :n_q].reshape(n, n_q * hd), equal_nan=True)
+        assert np.array_equal(bf16_host(K)[a:a + n], qk[:, n_q:].reshape(n, n_kv * hd), equal_nan=True)
+        if n:
+            OA.append(qk[:, n_q:], codes[0], scales[0], pages[i], c, page)
+            OA.append(x[a:a + n, n_q + n_kv:], codes[1], scales[1], pages[i], c, page)
+    for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+        assert np.array_equal(host(got), want)            # pages that nothing was added to among them
+    assert (bf16_host(Q)[rows:] == 7).all() and (bf16_host(K)[rows:] == 7).all()
+
+
+def test_append_token_by_token_grows_the_scale_as_the_oracle_does():
+    rng = np.random.default_rng(5)
+    n_q, n_kv, hd, page, n = 8, 2, 128, 16, 37
+    cache, pages, codes, scales = paged(rng, [n], page, n_kv, hd)
+    tab = table(n, hd)
+    qkv = bf16(rng, n, (n_q + 2 * n_kv) * hd) * torch.linspace(0.1, 5, n)[:, None].to(torch.bfloat16)
+    ws, tabd, dev = workspace(), torch.from_numpy(tab).to(DEV), qkv.to(DEV)
+    x = qkv.float().numpy().reshape(n, -1, hd)
+    for t in range(n):
+        B.fpt_rope_append(dev[t:t + 1], n_q, cache, tabd, i32([t]), ws=ws)
+        k = OA.rope(x[t:t + 1, n_q:n_q + n_kv], tab[t:t + 1], hd, False)
+        OA.append(k, codes[0], scales[0], pages[0], t, page)
+        OA.append(x[t:t + 1, n_q + n_kv:], codes[1], scales[1], pages[0], t, page)
+    assert B.fpt_check_status(ws) == B.OK
+    for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+        assert np.array_equal(host(got), want)
+
+
+def test_rotation_alone_and_in_place():
+    rng = np.random.default_rng(6)
+    n_q, n_kv, hd, new, ctx = 6, 2, 64, [3, 130], [10, 0]
+    x = bf16(rng, sum(new), (n_q + 2 * n_kv) * hd)
+    tab = table(140, 32)
+    dev, ws = x.to(DEV), workspace()
+    B.fpt_rope_append(dev, n_q, B.KVCache.heads(n_kv, hd), torch.from_numpy(tab).to(DEV), i32(ctx), cu_new=i32([0, 3, 133]),
+                      Q=dev[:, :n_q * hd], K=dev[:, n_q * hd:(n_q + n_kv) * hd], ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    got, want = bf16_host(dev).reshape(133, -1, hd), x.float().numpy().reshape(133, -1, hd)
+    pos = np.concatenate([np.arange(10, 13), np.arange(130)])
+    want[:, :n_q + n_kv] = OA.rope(want[:, :n_q + n_kv], tab[pos], 32, False)
+    assert np.array_equal(got, want)
+
+
+# ------------------------------------------------------------------------------------------------ gather
+@pytest.mark.parametrize("hd,page,n_kv,first,count", [
+    (128, 64, 8, [0, 3, 64], [64, 200, 1]), (128, 16, 1, [15, 0], [2, 0]), (64, 32, 3, [0, 31, 5], [1, 33, 100]),
+    (64, 128, 12, [100], [300]), (128, 128, 2, [0, 0, 127], [129, 0, 1])])
+def test_gather_gives_the_held_values(hd, page, n_kv, first, count):
+    rng = np.random.default_rng(7)
+    cache, pages, codes, scales = paged(rng, [f + c for f, c in zip(first, count)], page, n_kv, hd)
+    rows, ws = sum(count) + 2, workspace()
+    wide = guarded_empty((rows, 2 * n_kv * hd), torch.bfloat16)
+    wide.fill_(7.0)
+    K, V = wide[:, :n_kv * hd], wide[:, n_kv * hd:]
+    B.fpt_kv_gather(cache, i32(offsets(count).tolist()), rows, first=i32(first), K=K, V=V, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    for got, c, s in ((K, codes[0], scales[0]), (V, codes[1], scales[1])):
+        want = np.concatenate([OA.read(c, s, pages[i], f, n, page) for i, (f, n) in enumerate(zip(first, count))])
+        want = torch.from_numpy(want).to(torch.bfloat16).float().numpy().reshape(rows - 2, -1)
+        assert np.array_equal(bf16_host(got)[:-2], want) and (bf16_host(got)[-2:] == 7).all()
+
+
+# ------------------------------------------------------------------------------------------------ one token
+DECODE = [
+    # hd, page, n_q, n_kv, lengths
+    (128, 64, 32, 8, [1]),
+    (128, 64, 32, 8, [1000]),
+    (128, 64, 32, 8, [0, 1, 63, 64, 65, 127, 128, 129, 700]),
+    (128, 16, 4, 4, [17, 0, 5, 333, 16]),
+    (128, 32, 7, 1, [2000, 33, 1]),
+    (128, 128, 10, 2, [129, 1, 0, 257]),
+    (128, 64, 16, 1, [555, 64]),                 # 16 heads on one
+    (128, 64, 40, 2, [300, 20]),                 # 20: two blocks, the second of four
+    (128, 16, 64, 1, [77]),                      # 64: four blocks
+    (64, 64, 12, 12, [0, 2500, 1, 64]),
+    (64, 16, 9, 3, [100, 47, 15]),
+    (64, 32, 24, 2, [65, 400]),
+    (64, 128, 8, 1, [1000, 128]),
+]
+
+
+def decode_case(rng, hd, page, n_q, n_kv, lens, gain=1.0):
+    cache, pages, codes, scales = paged(rng, lens, page, n_kv, hd)
+    q = bf16(rng, len(lens), n_q * hd, gain=gain)
+    return cache, pages, codes, scales, q
+
+
+def check_decode(got, lse, lens, pages, codes, scales, q, n_q, hd, page, scale):
+    for i, n in enumerate(lens):
+        k, v = (OA.read(codes[j], scales[j], pages[i], 0, n, page) for j in (0, 1))
+        o, z, spread, mass = OA.attend(q[i].float().numpy().reshape(1, n_q, hd), k, v, scale, False)
+        close(bf16_host(got)[i].reshape(1, n_q, hd), o, out_bound(o, spread, mass, hd, 2.0 ** -11), f"sequence {i} of {n}")
+        if lse is not None:
+            close(host(lse)[i][None], z, lse_bound(z, mass, hd), f"lse of sequence {i}")
+
+
+@pytest.mark.parametrize("hd,page,n_q,n_kv,lens", DECODE)
+def test_decode(hd, page, n_q, n_kv, lens):
+    rng = np.random.default_rng(sum(lens) + hd)
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    ws = workspace()
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+    again, _ = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), ws=ws)       # the counters are back where they were
+    assert torch.equal(o.view(torch.int16), again.view(torch.int16))
+
+
+def test_decode_sharp_weights_and_uneven_scales():
+    """One key far above the others, maxima that keep growing along the sequence, pages whose scales lie far apart, a page of zeros."""
+    rng = np.random.default_rng(9)
+    hd, page, n_q, n_kv, lens = 128, 32, 8, 2, [900, 64]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens, gain=3.0)
+    for p, i in enumerate(pages[0]):
+        scales[0][i] *= 1.0 + 0.2 * p
+        scales[1][i] *= 10.0 ** (p % 7 - 3)
+    scales[1][pages[0][3]] = 0
+    codes[1][pages[0][3]] = 0
+    cache.k_scale.copy_(torch.from_numpy(scales[0])), cache.v_scale.copy_(torch.from_numpy(scales[1]))
+    cache.v.copy_(torch.from_numpy(codes[1]))
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True)
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+
+
+def test_decode_queries_of_any_size():
+    rng = np.random.default_rng(10)
+    hd, page, n_q, n_kv, lens = 64, 64, 4, 2, [200] * 4
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    q[1] *= 1e-30
+    q[2] = 0
+    q[3] *= 1e6
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), scale=1e-5, want_lse=True)
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, page, 1e-5)
+
+
+def test_decode_rows_in_wider_buffers():
+    rng = np.random.default_rng(11)
+    hd, page, n_q, n_kv, lens = 128, 64, 8, 2, [70, 300, 5]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    wide = torch.full((3, n_q * hd + 40), 5.0, dtype=torch.bfloat16)
+    wide[:, :n_q * hd] = q
+    out = guarded_empty((3, n_q * hd + 8), torch.bfloat16)
+    out.fill_(7.0)
+    o, _ = B.fpt_attn_decode(wide.to(DEV)[:, :n_q * hd], cache, i32(lens), O=out[:, :n_q * hd])
+    check_decode(o, None, lens, pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+    assert (bf16_host(out)[:, n_q * hd:] == 7).all()
+
+
+def test_decode_many_sequences():
+    """More sequences than one look at the lengths takes, more rows than CTAs."""
+    rng = np.random.default_rng(12)
+    hd, page, n_q, n_kv = 64, 16, 4, 4
+    lens = [int(n) for n in rng.integers(0, 150, 333)]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True)
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+
+
+def test_decode_page_out_of_range_is_recorded_and_spares_the_others():
+    rng = np.random.default_rng(13)
+    hd, page, n_q, n_kv, lens = 128, 16, 4, 2, [100, 40, 64]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    cache.pages[1, 1] = 1 << 30
+    ws = workspace()
+    o, _ = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), ws=ws)
+    assert B.fpt_check_status(ws) == B.ERR_INDEX
+    check_decode(o[0:1], None, lens[:1], pages[:1], codes, scales, q[:1], n_q, hd, page, hd ** -0.5)
+    check_decode(o[2:3], None, lens[2:], pages[2:], codes, scales, q[2:], n_q, hd, page, hd ** -0.5)
+    B.lib().fpt_reset_status(B._stream(), B._ptr(ws))
+    cache.pages[1, 1] = int(pages[1, 1])
+    B.fpt_attn_decode(q.to(DEV), cache, i32([100, 40, 1 << 28]), ws=ws)       # longer than its pages: cut to them
+    assert B.fpt_check_status(ws) == B.ERR_INDEX
+
+
+# ------------------------------------------------------------------------------------------------ prompts
+PROMPT = [
+    # hd, n_q, n_kv, len_q, len_k (None: the same), causal
+    (128, 32, 8, [1], None, True),
+    (128, 4, 1, [130], None, True),
+    (128, 4, 1, [64, 1, 127, 65, 128, 3], None, True),
+    (128, 8, 8, [129, 300], None, True),
+    (128, 7, 1, [200, 13], None, True),
+    (128, 12, 2, [100, 0, 50], None, True),
+    (128, 16, 1, [40, 9], None, True),
+    (128, 2, 2, [40, 300, 5], [300, 300, 700], True),        # chunks behind prefixes
+    (128, 4, 2, [100, 260, 7, 3], [20, 0, 3, 130], True),    # more queries than keys, no keys
+    (128, 4, 2, [100, 3], [333, 128], False),
+    (64, 24, 4, [257, 31], None, True),
+    (64, 3, 3, [128, 256, 511], None, True),
+    (64, 8, 1, [77, 5], [600, 129], True),
+    (64, 8, 2, [0, 300], [10, 200], False),
+    (128, 4, 4, [1100], None, True),                          # the ring of tiles more than once around
+    (64, 4, 4, [1300], [1700], True),
+]
+
+
+def prompt_case(rng, hd, n_q, n_kv, len_q, len_k, pad=5):
+    return (bf16(rng, sum(len_q) + pad, n_q * hd), bf16(rng, sum(len_k) + pad, n_kv * hd, gain=1.5),
+            bf16(rng, sum(len_k) + pad, n_kv * hd))
+
+
+def check_prompt(got, lse, q, k, v, n_q, n_kv, hd, len_q, len_k, causal, scale=None):
+    a, b = offsets(len_q), offsets(len_k)
+    for i in range(len(len_q)):
+        args = [t.float().numpy()[x[i]:x[i + 1]].reshape(x[i + 1] - x[i], -1, hd) for t, x in ((q, a), (k, b), (v, b))]
+        o, z, spread, mass = OA.attend(*args, hd ** -0.5 if scale is None else scale, causal)
+        close(bf16_host(got)[a[i]:a[i + 1]].reshape(o.shape), o, out_bound(o, spread, mass, hd, HALF), f"sequence {i}")
+        if lse is not None:
+            close(host(lse)[a[i]:a[i + 1]], z, lse_bound(z, mass, hd), f"lse of sequence {i}")
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,len_q,len_k,causal", PROMPT)
+def test_prompt(hd, n_q, n_kv, len_q, len_k, causal):
+    same, len_k = len_k is None, len_k or len_q
+    rng = np.random.default_rng(sum(len_q) + hd + n_q)
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, len_q, len_k)
+    k[sum(len_k):] = math.nan                            # rows behind the last sequence
+    v[sum(len_k):] = math.inf
+    rows = sum(len_q)
+    out = guarded_empty(q.shape, torch.bfloat16)
+    out.fill_(7.0)
+    ws = workspace()
+    _, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32(offsets(len_q).tolist()),
+                               cu_k=None if same else i32(offsets(len_k).tolist()), causal=causal, want_lse=True, O=out, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_prompt(out, lse, q, k, v, n_q, n_kv, hd, len_q, len_k, causal)
+    assert (bf16_host(out)[rows:] == 7).all()
+
+
+def test_prompt_from_one_buffer():
+    """Queries, keys and values as places of one projection's rows; the output in a wider buffer."""
+    rng = np.random.default_rng(21)
+    hd, n_q, n_kv, lens = 128, 8, 2, [150, 33]
+    x = bf16(rng, sum(lens), (n_q + 2 * n_kv) * hd + 16)
+    d = x.to(DEV)
+    cut = [(0, n_q * hd), (n_q * hd, (n_q + n_kv) * hd), ((n_q + n_kv) * hd, (n_q + 2 * n_kv) * hd)]
+    out = guarded_empty((sum(lens), n_q * hd + 8), torch.bfloat16)
+    out.fill_(7.0)
+    B.fpt_attn_prompt(*(d[:, a:b] for a, b in cut), n_q, n_kv, i32([0, 150, 183]), O=out[:, :n_q * hd])
+    check_prompt(out[:, :n_q * hd], None, *(x[:, a:b] for a, b in cut), n_q, n_kv, hd, lens, lens, True)
+    assert (bf16_host(out)[:, n_q * hd:] == 7).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_maxima_that_grow_and_sharp_weights(hd):
+    """Scores that climb along the keys: every tile renews the maximum and turns the sums in tensor memory down."""
+    rng = np.random.default_rng(22)
+    n_q, n_kv, lens = 2, 1, [700]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, lens, lens, pad=0)
+    q.fill_(1.0)
+    k.copy_((torch.linspace(-1, 1, 700)[:, None] * 40 / hd ** 0.5 + 0.02 * torch.randn(700, hd, generator=torch.Generator().manual_seed(1))).to(torch.bfloat16))
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32([0, 700]), want_lse=True)
+    check_prompt(o, lse, q, k, v, n_q, n_kv, hd, lens, lens, True)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_odd_values_reach_only_who_sees_them(hd):
+    """Infinities and NaN among keys and values: queries in front of them, and other sequences, are untouched."""
+    rng = np.random.default_rng(23)
+    n_q, n_kv, lens = 4, 2, [200, 70, 30]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, lens, lens, pad=0)
+    v[150, 3] = math.inf
+    v[190, 3] = -math.inf
+    v[199, hd + 1] = math.nan
+    k[180, hd:] = math.nan                               # the second key head
+    v[260, :] = math.nan
+    k[205, 0] = math.inf
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32(offsets(lens).tolist()), want_lse=True)
+    got = bf16_host(o)
+    # the oracle leaves hidden keys and values out row by row; where a value that is not finite is seen, so is the result
+    a = offsets(lens)
+    for i in range(3):
+        args = [t.float().numpy()[a[i]:a[i + 1]].reshape(lens[i], -1, hd) for t in (q, k, v)]
+        want, _, spread, mass = OA.attend(*args, hd ** -0.5, True)
+        mine = got[a[i]:a[i + 1]].reshape(want.shape)
+        fine = np.isfinite(want)
+        assert (np.isfinite(mine) == fine).all(), i
+        assert (np.abs(mine - want)[fine] <= out_bound(want, spread, mass, hd, HALF)[fine]).all(), i
+
+
+def test_prompt_offsets_out_of_range_are_recorded():
+    rng = np.random.default_rng(24)
+    q, k, v = (t.to(DEV) for t in prompt_case(rng, 64, 2, 1, [100], [100], pad=0))
+    for cu in ([0, 101], [0, -5], [-3, 40], [50, 20]):
+        ws = workspace()
+        out = guarded_empty(q.shape, torch.bfloat16)
+        B.fpt_attn_prompt(q, k, v, 2, 1, i32(cu), O=out, ws=ws)
+        B.fpt_attn_prompt(q, k, v, 2, 1, i32([0, 100]), cu_k=i32(cu), O=out, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX, cu
+
+
+# ------------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("hd,page,inter", [(128, 64, False), (64, 16, True)])
+def test_a_prompt_in_chunks_and_single_tokens_agree(hd, page, inter):
+    """The run of a server: a prompt in two chunks (append, prefix in 16 bits, attention), then tokens one at a time."""
+    rng = np.random.default_rng(31)
+    n_q, n_kv, lens, steps = 8, 2, [90, 33], 3
+    total = [n + steps for n in lens]
+    cache, pages, codes, scales = paged(rng, total, page, n_kv, hd, filled=False)
+    tab = table(max(total), hd)
+    tabd, ws = torch.from_numpy(tab).to(DEV), workspace()
+    layout = B.ROPE_INTERLEAVED if inter else B.ROPE_HALF
+    x = [bf16(rng, n, (n_q + 2 * n_kv) * hd) for n in total]
+    have = [0, 0]
+    plan = [[50, 20], [40, 13]] + [[1, 1]] * steps
+    for new in plan:
+        rows = torch.cat([x[i][have[i]:have[i] + n] for i, n in enumerate(new)]).to(DEV)
+        ends = [h + n for h, n in zip(have, new)]
+        cu = i32(offsets(new).tolist())
+        single = new == [1, 1]
+        q, _ = B.fpt_rope_append(rows, n_q, cache, tabd, i32(have), cu_new=None if single else cu, layout=layout, ws=ws)
+        if single:
+            o, _ = B.fpt_attn_decode(q, cache, i32(ends), ws=ws)
+        else:
+            cu_k = i32(offsets(ends).tolist())
+            k, v = B.fpt_kv_gather(cache, cu_k, sum(ends), ws=ws)
+            o, _ = B.fpt_attn_prompt(q, k, v, n_q, n_kv, cu, cu_k=cu_k, ws=ws)
+        assert B.fpt_check_status(ws) == B.OK
+        a = offsets(new)
+        for i, n in enumerate(new):
+            y = x[i].float().numpy().reshape(total[i], -1, hd)
+            qk = OA.rope(y[have[i]:ends[i], :n_q + n_kv], tab[have[i]:ends[i]], hd, inter)
+            OA.append(qk[:, n_q:], codes[0], scales[0], pages[i], have[i], page)
+            OA.append(y[have[i]:ends[i], n_q + n_kv:], codes[1], scales[1], pages[i], have[i], page)
+            kk, vv = (OA.read(codes[j], scales[j], pages[i], 0, ends[i], page) for j in (0, 1))
+            if not single:
+                kk, vv = (torch.from_numpy(t).to(torch.bfloat16).float().numpy() for t in (kk, vv))
+            want, _, spread, mass = OA.attend(qk[:, :n_q], kk, vv, hd ** -0.5, True)
+            close(bf16_host(o)[a[i]:a[i + 1]].reshape(want.shape), want,
+                  out_bound(want, spread, mass, hd, 2.0 ** -11 if single else HALF), f"sequence {i} at {have[i]}")
+        have = ends
+    for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+        assert np.array_equal(host(got), want)
