@@ -65,7 +65,7 @@ def attend(q, k, v, scale, causal):
     lse, mass = np.full((lq, nq), -np.inf), np.zeros((lq, nq))
     seen = np.clip(np.arange(lq) + lk - lq + 1, 0, lk) if causal else np.full(lq, lk)
     mask = np.arange(lk)[None, :] < seen[:, None]
-    for h in range(nkv if lk else 0):
+    for h in range(nkv if lq and lk else 0):
         sl = slice(h * g, (h + 1) * g)
         for rows in ([slice(0, lq)] if np.isfinite(k[:, h]).all() and np.isfinite(v[:, h]).all() else
                      [slice(i, i + 1) for i in range(lq)]):             # one at a time: what is hidden is left out, not weighted

@@ -42,8 +42,8 @@ struct PrSmem {
   static constexpr int kHalf = kPrTile * 128;                // 64 of its columns: 128-byte rows
   static constexpr int kKvOff = 2 * kMat;
   static constexpr int kBarOff = kKvOff + kStages * kMat;
-  static constexpr int kNumBars = 2 + 2 * kStages + 2 + 2 + 2 + 1;
-  static constexpr int kMiscOff = kBarOff + kNumBars * 8 + 8;
+  static constexpr int kNumBars = 2 + 4 * kStages + 2 + 2 + 2;
+  static constexpr int kMiscOff = (kBarOff + kNumBars * 8 + 15) / 16 * 16;
   static constexpr int kAlloc = kMiscOff + 32 + 1024;
 };
 
@@ -145,7 +145,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto s_full = [&](int w) { return bar0 + 8u * (2 + 2 * ST + w); };
   auto p_full = [&](int w) { return bar0 + 8u * (4 + 2 * ST + w); };
   auto o_full = [&](int w) { return bar0 + 8u * (6 + 2 * ST + w); };
-  const uint32_t v_clean = bar0 + 8u * (8 + 2 * ST);
+  // values of a cut tile: arrived (for the warps that clean them), clean.  One of each a stage: a stage is not filled
+  // again before the tensor core has read it, so no phase of theirs is over before it was waited for
+  auto v_raw = [&](int s) { return bar0 + 8u * (8 + 2 * ST + s); };
+  auto v_clean = [&](int s) { return bar0 + 8u * (8 + 3 * ST + s); };
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + L::kMiscOff);
   volatile uint32_t* abort_flag = misc + 1;
   volatile uint32_t* odd_values = misc + 2;                  // a cut tile's values were not all finite
@@ -203,8 +206,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       mbar_init(p_full(i), 4);
       mbar_init(o_full(i), 1);
     }
-    for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 1); }
-    mbar_init(v_clean, 2);
+    for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 1); mbar_init(v_raw(i), 1); mbar_init(v_clean(i), 2); }
     misc[1] = 0;
     misc[2] = 0;
     fence_mbar_init();
@@ -345,28 +347,34 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           for (int h = 0; h < HD / 64; ++h)
             tma_load_3d(sbase + i * L::kMat + h * L::kHalf, &tmQ, q_full(i), h * 64, head0, row0 + tok0 + i * per_tile);
         };
-        auto fetch = [&](const CUtensorMap* tm, int j) {
+        uint32_t raw_par = 0;                                 // per stage: parity of the next phase of v_raw
+        auto fetch = [&](const CUtensorMap* tm, int j, bool clean) {
           if (!mbar_wait(kv_empty(st), ph ^ 1u, abort_flag, P.status, 1)) return false;
-          mbar_arrive_expect_tx(kv_full(st), L::kMat);
+          // values to be cleaned arrive on a barrier of their own, whose every phase the cleaning warps see
+          const uint32_t bar = clean ? v_raw(st) : kv_full(st);
+          if (clean) mbar_arrive(kv_full(st));
+          mbar_arrive_expect_tx(bar, L::kMat);
 #pragma unroll
           for (int h = 0; h < HD / 64; ++h)
-            tma_load_2d(sbase + L::kKvOff + st * L::kMat + h * L::kHalf, tm, kv_full(st), kv_head * HD + h * 64,
-                        key0 + j * kPrTile);
-          armed |= 1u << st;
-          armed_par = (armed_par & ~(1u << st)) | (ph << st);
+            tma_load_2d(sbase + L::kKvOff + st * L::kMat + h * L::kHalf, tm, bar, kv_head * HD + h * 64, key0 + j * kPrTile);
+          const int slot = clean ? ST + st : st;
+          armed |= 1u << slot;
+          armed_par = (armed_par & ~(1u << slot)) | ((clean ? raw_par >> st & 1u : ph) << slot);
+          if (clean) raw_par ^= 1u << st;
           if (++st == ST) { st = 0; ph ^= 1u; }
           return true;
         };
         queries(0);
-        ok = fetch(&tmK, 0);
+        ok = fetch(&tmK, 0, false);
         if (two) queries(1);
-        ok = ok && fetch(&tmV, 0);
-        for (int j = 1; ok && j < tiles; ++j) ok = fetch(&tmK, j) && fetch(&tmV, j);
+        ok = ok && fetch(&tmV, 0, cut == 0);
+        for (int j = 1; ok && j < tiles; ++j) ok = fetch(&tmK, j, false) && fetch(&tmV, j, j >= cut);
         if (!ok) {
           const uint64_t t0 = globaltimer_ns();
-          for (int i = 0; i < ST; ++i)
+          for (int i = 0; i < 2 * ST; ++i)
             if (armed & (1u << i))
-              while (!mbar_try_wait(kv_full(i), (armed_par >> i) & 1u) && globaltimer_ns() - t0 < 2000000ull) {}
+              while (!mbar_try_wait(i < ST ? kv_full(i) : v_raw(i - ST), (armed_par >> i) & 1u) &&
+                     globaltimer_ns() - t0 < 2000000ull) {}
         }
       }
     } else if (warp == 9) {
@@ -376,6 +384,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const int nw = two ? 2 : 1;
         int st = 0; uint32_t ph = 0;                          // ring: keys 0, values 0, keys 1, ...
         int k_st = 0, v_st = 0;
+        uint32_t clean_par = 0;                               // per stage: parity of the next phase of v_clean
         bool ok = true;
         auto next = [&](int& mine) {
           mine = st;
@@ -401,7 +410,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (ok) umma_commit(kv_empty(k_st));
         for (int j = 0; ok && j < tiles; ++j) {
           ok = next(v_st);
-          if (ok && j >= cut) ok = mbar_wait(v_clean, (j - cut) & 1, abort_flag, P.status, 3);
+          if (ok && j >= cut) {
+            ok = mbar_wait(v_clean(v_st), (clean_par >> v_st) & 1u, abort_flag, P.status, 3);
+            clean_par ^= 1u << v_st;
+          }
           if (ok && j + 1 < tiles) ok = next(k_st);
           for (int i = 0; ok && i < nw; ++i) {
             ok = mbar_wait(p_full(i), j & 1, abort_flag, P.status, 3);
@@ -422,9 +434,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
     } else {
       // ---------------------------------------------------------------- values of the cut tiles
+      uint32_t raw_par = 0;
       for (int j = cut; j < tiles; ++j) {
-        const int n = 2 * j + 1, st = n % ST;                 // place in the ring
-        if (!mbar_wait_warp(kv_full(st), (n / ST) & 1, abort_flag, P.status, 6)) break;
+        const int st = (2 * j + 1) % ST;                      // place in the ring
+        if (!mbar_wait_warp(v_raw(st), (raw_par >> st) & 1u, abort_flag, P.status, 6)) break;
+        raw_par ^= 1u << st;
         uint8_t* v = smem + L::kKvOff + st * L::kMat;
         bool odd = false;
         for (int i = (warp - 10) * 32 + lane; i < L::kMat / 16; i += 64) {
@@ -450,7 +464,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (odd) *odd_values = 1;
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(v_clean);
+        if (lane == 0) mbar_arrive(v_clean(st));
       }
     }
   }

@@ -64,7 +64,7 @@ def close(got, want, bound, what):
     fine = np.isfinite(want)
     assert (np.isfinite(got) == fine).all(), f"{what}: finite in other places"
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
-    off = np.abs(got - want)[fine] - np.broadcast_to(bound, want.shape)[fine]
+    off = np.abs(got[fine] - want[fine]) - np.broadcast_to(bound, want.shape)[fine]
     assert off.size == 0 or off.max() <= 0, f"{what}: {int((off > 0).sum())} of {off.size} off, worst by {off.max():.3g}"
 
 
@@ -337,7 +337,7 @@ def prompt_case(rng, hd, n_q, n_kv, len_q, len_k, pad=5):
 def check_prompt(got, lse, q, k, v, n_q, n_kv, hd, len_q, len_k, causal, scale=None):
     a, b = offsets(len_q), offsets(len_k)
     for i in range(len(len_q)):
-        args = [t.float().numpy()[x[i]:x[i + 1]].reshape(x[i + 1] - x[i], -1, hd) for t, x in ((q, a), (k, b), (v, b))]
+        args = [t.float().numpy()[x[i]:x[i + 1]].reshape(x[i + 1] - x[i], t.shape[1] // hd, hd) for t, x in ((q, a), (k, b), (v, b))]
         o, z, spread, mass = OA.attend(*args, hd ** -0.5 if scale is None else scale, causal)
         close(bf16_host(got)[a[i]:a[i + 1]].reshape(o.shape), o, out_bound(o, spread, mass, hd, HALF), f"sequence {i}")
         if lse is not None:
