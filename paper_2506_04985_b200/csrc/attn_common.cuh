@@ -29,6 +29,41 @@ __device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float 
   return __byte_perm(__byte_perm(code_of(a), code_of(b), 0x0040u), __byte_perm(code_of(c), code_of(d), 0x0040u), 0x5410u);
 }
 
+// The bounded waits of fpt_common.cuh with a suspend hint: these kernels have up to sixteen warps that wait most of the time, and
+// without the hint the instruction comes back at once, so that the polling takes issue slots from the warps that work.
+__device__ __forceinline__ uint32_t mbar_try_wait_long(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity), "r"(20000u)
+      : "memory");
+  return done;
+}
+template <bool WARP>
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status, uint32_t role) {
+  auto done = [&]() -> bool {
+    const uint32_t d = mbar_try_wait_long(bar, parity);
+    return WARP ? __all_sync(0xffffffffu, d) : d != 0;
+  };
+  if (done()) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (;;) {
+    if (done()) return true;
+    const bool late = globaltimer_ns() - t0 > kWaitLimitNs;
+    const bool give_up = late || *abort_flag;
+    if (WARP ? __any_sync(0xffffffffu, give_up) : give_up) {
+      if (late) {
+        *abort_flag = 1u;
+        atomicCAS(status, 0u, kStatusTimeoutBase | role);
+      }
+      return false;
+    }
+  }
+}
+
 // What a page's codes are multiplied with before rounding.
 __device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435e-38f ? __fdiv_rn(1.0f, s) : 0.0f; }
 

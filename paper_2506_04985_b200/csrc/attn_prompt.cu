@@ -1,29 +1,62 @@
 // Causal attention of packed prompts (fpt_attn_prompt; formulas: include/fpt.h).
 //
-// One CTA has two tiles of 128 query rows of one key/value head and walks over that head's keys in tiles of 128.  A row
+// A task is two tiles of 128 query rows of one key/value head, and a walk over that head's keys in tiles of 128.  A row
 // is a (token, query head of the group) pair: as many heads of the group as divide 128 share a tile, so a prompt of few
-// tokens still fills it, and the keys are fetched once for all of them.
+// tokens still fills it, and the keys are fetched once for all of them.  The grid has a CTA a task, in the order of a sequence's
+// last rows first (with a causal mask, the longest); a CTA that has requested all of its task's keys takes over one that was
+// not started yet (cluster launch control), so that the loads, the look-ups and the first scores of the next task run under the last
+// tiles and the epilogue of this one, and a long task keeps nobody waiting.
 //   warps 0..3, 4..7   softmax of the first and the second query tile, one row a thread
-//   warp 8             TMA: queries once, keys and values through a ring
-//   warp 9             tensor core:  S = Q K^T (both from shared memory),  O += P V (P from tensor memory, V as it lies: the
+//   warps 8..11        the end of a task: O from tensor memory, divided, to its rows, while the softmax is at the next task
+//   warp 12            the next task; TMA: queries once a task, keys and values through a ring
+//   warp 13            tensor core:  S = Q K^T (both from shared memory),  O += P V (P from tensor memory, V as it lies: the
 //                      instruction takes it with the keys along the rows)
-//   warps 10, 11       values of the tiles that a mask cuts: those that are not finite become zeros before the tensor core
+//   warps 14, 15       values of the tiles that a mask cuts: those that are not finite become zeros before the tensor core
 //                      reads them (a weight of zero would not make them harmless), as do rows behind the sequence
 // While the softmax of one tile runs, the tensor core works for the other.  P (bf16) takes the place of S in tensor
 // memory; the next S of a tile is issued behind the P V that reads it, and the tensor core keeps that order.
 //
 // Softmax in the exponent of two: p = 2^(S scale log2(e) - m).  m is the row's maximum when it was last renewed: it is renewed, and O in
 // tensor memory multiplied by 2^(m_old - m_new), only where the maximum has grown by more than 8, so that p <= 256; the quotient by
-// the sum of weights is the same for any m.  In tiles without a mask a part of the powers is computed by a polynomial
-// on the multiply-add units, since the special-function unit would be the slower side.
+// the sum of weights is the same for any m.
+// (A part of the powers as a polynomial on the multiply-add units, since 128 powers a row keep the special-function unit busy half
+// as long as the tensor core works on a tile: 3 % slower at a quarter of them, 13 % at half.)
+#include <type_traits>
+
 #include "attn_common.cuh"
 
 namespace fpt {
 
 constexpr int kPrTile = 128;               // query rows of a tile, keys of a tile
-constexpr int kPrThreads = 384;
-constexpr int kPrSoftRegs = 208, kPrAuxRegs = 88;
-static_assert(2 * 128 * kPrSoftRegs + 128 * kPrAuxRegs <= kPrThreads * 168, "the warpgroups' registers exceed the launch's");
+constexpr int kPrThreads = 512;
+constexpr int kPrSoftRegs = 176, kPrEndRegs = 80, kPrAuxRegs = 80;
+static_assert(128 * (2 * kPrSoftRegs + kPrEndRegs + kPrAuxRegs) <= kPrThreads * 128, "the warpgroups' registers exceed the launch's");
+constexpr int kPrEarly = 6;                // of the eight 16-key steps of P V, those that begin before the last weights are there
+
+// Lane l of four: y[i] becomes y[l & 3] of lane (l & ~3) + i.  (Written out: an index that the compiler does not see through
+// would put y into local memory, and with 227 KB of shared memory there is hardly a cache behind it.)
+__device__ __forceinline__ void swap_lanes(uint4& a, uint4& b, bool up, int m) {
+  uint32_t* x = &a.x;
+  uint32_t* y = &b.x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x[k] : y[k], m);
+    x[k] = up ? got : x[k];
+    y[k] = up ? y[k] : got;
+  }
+}
+__device__ __forceinline__ void transpose4(uint4 (&y)[4], int lane) {
+  swap_lanes(y[0], y[1], lane & 1, 1);
+  swap_lanes(y[2], y[3], lane & 1, 1);
+  swap_lanes(y[0], y[2], lane & 2, 2);
+  swap_lanes(y[1], y[3], lane & 2, 2);
+}
+
+struct __align__(16) TaskInfo {
+  int row0, len_q, key0, len_k;       // the sequence
+  int tok0, tiles, cut, flags;        // first token; tiles of keys; tiles from `cut` on are masked for some row; 1: a task, 2: the second query tile has rows
+  int head0, kv_head, odd, pad;       // odd: a cut tile's values were not all finite
+};
 
 struct PromptParams {
   const int32_t *cu_q, *cu_k;
@@ -31,7 +64,7 @@ struct PromptParams {
   __nv_bfloat16* O;
   float* lse;
   uint32_t* status;
-  int ld_v, ld_o, M_q, M_k, n_q, n_kv, group, pack, units, n_seqs, n_tasks, causal;
+  int ld_v, ld_o, M_q, M_k, n_q, n_kv, group, pack_log2, units, n_seqs, n_tasks, causal;
   float scale_log2;
 };
 
@@ -42,9 +75,11 @@ struct PrSmem {
   static constexpr int kHalf = kPrTile * 128;                // 64 of its columns: 128-byte rows
   static constexpr int kKvOff = 2 * kMat;
   static constexpr int kBarOff = kKvOff + kStages * kMat;
-  static constexpr int kNumBars = 2 + 4 * kStages + 2 + 2 + 2;
+  static constexpr int kNumBars = 4 + 4 * kStages + 2 + 4 + 4 + 5 + 4;
   static constexpr int kMiscOff = (kBarOff + kNumBars * 8 + 15) / 16 * 16;
-  static constexpr int kAlloc = kMiscOff + 32 + 1024;
+  static constexpr int kInfoOff = kMiscOff + 32;             // (16 bytes of misc, the answer of the launch control)
+  static constexpr int kStatOff = kInfoOff + 2 * 48;         // [query tile][row] {maximum, sum of weights}
+  static constexpr int kAlloc = kStatOff + 2 * kPrTile * 8;
 };
 
 // Shared-memory matrix descriptor of a B operand that lies with its rows along k (128-byte rows of 64 columns, 128-byte
@@ -104,29 +139,123 @@ __device__ __forceinline__ float pow2_unit(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-// 2^a, 2^b for a, b in [-126, 127): x = n + f with n the nearest integer (left in the low bits by the sum with 1.5 * 2^23),
-// 2^f by the polynomial of degree 4 with the least largest relative error on [-1/2, 1/2] (2.7e-6, 4e-8 in the
-// mean; found by reweighted least squares), n added to the exponent.
-__device__ __forceinline__ void pow2_poly(float& a, float& b) {
-  const uint64_t magic = pack2(12582912.0f, 12582912.0f), back = pack2(-12582912.0f, -12582912.0f);
-  const uint64_t x = pack2(fmaxf(a, -126.0f), fmaxf(b, -126.0f));
-  const uint64_t t = add2(x, magic);
-  const uint64_t n = add2(t, back);
-  const uint64_t f = fma2(n, pack2(-1.0f, -1.0f), x);
-  uint64_t p = fma2(f, pack2(0.009570102207362652f, 0.009570102207362652f), pack2(0.05591786280274391f, 0.05591786280274391f));
-  p = fma2(f, p, pack2(0.240247443318367f, 0.240247443318367f));
-  p = fma2(f, p, pack2(0.6931217908859253f, 0.6931217908859253f));
-  p = fma2(f, p, pack2(0.9999992847442627f, 0.9999992847442627f));
-  float t0, t1, p0, p1;
-  unpack2(t, t0, t1);
-  unpack2(p, p0, p1);
-  a = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  b = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+// Cluster launch control: asks for a block of this grid that was not started yet (it then never is); the answer, 16 bytes in
+// shared memory, counts on the barrier.  Not to be asked again after a refusal.
+__device__ __forceinline__ void ask_for_a_block(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(answer), "r"(bar) : "memory");
+}
+// Its blockIdx.x, or -1.
+__device__ __forceinline__ int block_of_answer(uint32_t answer) {
+  int x = -1;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
+      "ld.shared.b128 a, [%1];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "mov.b32 %0, -1;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
+      : "=r"(x)
+      : "r"(answer)
+      : "memory");
+  return x;
+}
+
+// Up to 32 sequences are taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short:
+// lane s knows where the tasks of sequence s begin and how many they are.
+struct TaskOrder { int first, count; };
+__device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane) {
+  TaskOrder o = {0, 0};
+  if (P.n_seqs > 32) return o;
+  int keys = -1;
+  if (lane < P.n_seqs) {
+    const int len_q = __ldg(P.cu_q + lane + 1) - __ldg(P.cu_q + lane), len_k = __ldg(P.cu_k + lane + 1) - __ldg(P.cu_k + lane);
+    o.count = max(0, len_q + ((256 >> P.pack_log2) - 1)) >> (8 - P.pack_log2);
+    keys = max(0, len_k);
+  }
+  for (int s = 0; s < P.n_seqs; ++s) {
+    const int k = __shfl_sync(0xffffffffu, keys, s), c = __shfl_sync(0xffffffffu, o.count, s);
+    if (k > keys || (k == keys && s < lane)) o.first += c;
+  }
+  return o;
+}
+
+// The task of block `bid`; whole warp, the same answer in every lane.  With more sequences than lanes, sequence s has
+// floor(cu_q[s+1] / per) - floor(cu_q[s] / per) + 1 tasks (at least the blocks of `per` rows that it needs), and which s a task belongs to
+// is found 32 places at a time.
+__device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const TaskOrder& order, int bid, int lane, TaskInfo& ti) {
+  const int per_log2 = 8 - P.pack_log2, per = 1 << per_log2;
+  const int turn = bid / P.units, unit = bid - turn * P.units;
+  int lo = 0, place;
+  if (P.n_seqs <= 32) {
+    const uint32_t mine = __ballot_sync(0xffffffffu, turn >= order.first && turn < order.first + order.count);
+    if (mine == 0) return false;
+    lo = __ffs(mine) - 1;
+    place = __shfl_sync(0xffffffffu, order.first + order.count, lo) - 1 - turn;      // last rows first
+  } else {
+    const int id = P.n_tasks - 1 - turn;
+    int hi = P.n_seqs;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const uint32_t below = __ballot_sync(0xffffffffu, at < hi && (__ldg(P.cu_q + min(at, hi - 1)) >> per_log2) + at <= id);
+      if (below) lo += (31 - __clz(below)) * step;
+      hi = min(hi, lo + step);
+    }
+    place = id - ((__ldg(P.cu_q + lo) >> per_log2) + lo);
+  }
+  ti.row0 = __ldg(P.cu_q + lo);
+  const int end_q = __ldg(P.cu_q + lo + 1);
+  ti.len_q = end_q - ti.row0;
+  ti.key0 = __ldg(P.cu_k + lo);
+  const int end_k = __ldg(P.cu_k + lo + 1);
+  ti.len_k = end_k - ti.key0;
+  if (ti.row0 < 0 || end_q < ti.row0 || end_q > P.M_q || ti.key0 < 0 || end_k < ti.key0 || end_k > P.M_k) {
+    if (lane == 0) record_bad_index(P.status, kBadOffset);
+    return false;
+  }
+  if (place < 0 || place >= (ti.len_q + per - 1) >> per_log2) return false;
+  ti.tok0 = place * per;
+  const int packs = P.group >> P.pack_log2;
+  ti.kv_head = unit / packs;
+  ti.head0 = ti.kv_head * P.group + ((unit - ti.kv_head * packs) << P.pack_log2);
+  const int ahead = ti.len_k - ti.len_q, last = min(ti.tok0 + per, ti.len_q) - 1;
+  const int seen_first = P.causal ? max(0, min(ti.len_k, ti.tok0 + ahead + 1)) : ti.len_k;
+  const int seen_last = P.causal ? max(0, min(ti.len_k, last + ahead + 1)) : ti.len_k;
+  ti.tiles = (seen_last + kPrTile - 1) / kPrTile;
+  ti.cut = seen_first / kPrTile;
+  ti.flags = 1 | (ti.tok0 + per / 2 < ti.len_q ? 2 : 0);
+  ti.odd = 0;
+  return true;
+}
+
+// What the zeros in the cut tiles stand for: a value that is not finite outweighs every finite sum, whatever its weight.
+__device__ __noinline__ void add_odd_values(const __nv_bfloat16* V, int ld, int hd, int from, int to, __nv_bfloat16* o) {
+  for (int d = 0; d < hd; ++d) {
+    float sum = __bfloat162float(o[d]);
+    for (int k = from; k < to; ++k) {
+      const float z = __bfloat162float(V[(size_t)k * ld + d]);
+      if (!(fabsf(z) < INFINITY)) sum += z;
+    }
+    if (!(fabsf(sum) < INFINITY)) o[d] = __float2bfloat16_rn(sum);
+  }
 }
 
 template <int HD>
@@ -135,86 +264,63 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                    const __grid_constant__ CUtensorMap tmV, const PromptParams P) {
   using L = PrSmem<HD>;
   constexpr int ST = L::kStages;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) uint8_t smem_tiles[];    // (no room to align it by hand: 227 KB are full)
+  uint8_t* smem = smem_tiles;
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar0 = sbase + L::kBarOff;
   auto q_full = [&](int w) { return bar0 + 8u * w; };
-  auto kv_full = [&](int s) { return bar0 + 8u * (2 + s); };
-  auto kv_empty = [&](int s) { return bar0 + 8u * (2 + ST + s); };
-  auto s_full = [&](int w) { return bar0 + 8u * (2 + 2 * ST + w); };
-  auto p_full = [&](int w) { return bar0 + 8u * (4 + 2 * ST + w); };
-  auto o_full = [&](int w) { return bar0 + 8u * (6 + 2 * ST + w); };
+  auto q_empty = [&](int w) { return bar0 + 8u * (2 + w); };
+  auto kv_full = [&](int s) { return bar0 + 8u * (4 + s); };
+  auto kv_empty = [&](int s) { return bar0 + 8u * (4 + ST + s); };
   // values of a cut tile: arrived (for the warps that clean them), clean.  One of each a stage: a stage is not filled
   // again before the tensor core has read it, so no phase of theirs is over before it was waited for
-  auto v_raw = [&](int s) { return bar0 + 8u * (8 + 2 * ST + s); };
-  auto v_clean = [&](int s) { return bar0 + 8u * (8 + 3 * ST + s); };
+  auto v_raw = [&](int s) { return bar0 + 8u * (4 + 2 * ST + s); };
+  auto v_clean = [&](int s) { return bar0 + 8u * (4 + 3 * ST + s); };
+  const uint32_t bar1 = bar0 + 8u * (4 + 4 * ST);
+  auto s_full = [&](int w) { return bar1 + 8u * w; };
+  auto p_full = [&](int w, int part) { return bar1 + 8u * (2 + 2 * w + part); };   // part: the first kPrEarly steps, the others
+  auto o_full = [&](int w) { return bar1 + 8u * (6 + w); };                        // a task's last P V
+  auto o_empty = [&](int w) { return bar1 + 8u * (8 + w); };
+  auto info_full = [&](int i) { return bar1 + 8u * (10 + i); };
+  auto info_empty = [&](int i) { return bar1 + 8u * (12 + i); };
+  auto stat_full = [&](int w) { return bar1 + 8u * (14 + w); };
+  auto stat_empty = [&](int w) { return bar1 + 8u * (16 + w); };
+  const uint32_t answered = bar1 + 8u * 18;
+  float2* stats = reinterpret_cast<float2*>(smem + L::kStatOff);
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + L::kMiscOff);
   volatile uint32_t* abort_flag = misc + 1;
-  volatile uint32_t* odd_values = misc + 2;                  // a cut tile's values were not all finite
-  int* found = reinterpret_cast<int*>(smem + L::kMiscOff + 16);
+  TaskInfo* infos = reinterpret_cast<TaskInfo*>(smem + L::kInfoOff);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_wait();
   pdl_launch_dependents();
-
-  // ---- which rows
-  const int per_tile = kPrTile / P.pack, per_cta = 2 * per_tile;          // tokens
-  int place;
-  const int s = find_task(P.cu_q, P.n_seqs, per_cta, 1, P.n_tasks - 1 - (int)(blockIdx.x / P.units), found, P.status, place);
-  if (s < 0) return;
-  const int row0 = __ldg(P.cu_q + s), len_q = __ldg(P.cu_q + s + 1) - row0;
-  const int key0 = __ldg(P.cu_k + s), key1 = __ldg(P.cu_k + s + 1);
-  const int len_k = key1 - key0;
-  if (row0 > P.M_q - len_q || key0 < 0 || len_k < 0 || key0 > P.M_k - len_k) {
-    if (threadIdx.x == 0) record_bad_index(P.status, kBadOffset);
+  if (sbase & 1023u) {                                       // not what was declared: no tile could be addressed
+    if (threadIdx.x == 0) atomicCAS(P.status, 0u, kStatusTimeoutBase | 15u);
     return;
   }
-  const int tok0 = place * per_cta;
-  if (place < 0 || tok0 >= len_q) return;
-  const int unit = blockIdx.x % P.units, packs = P.group / P.pack;
-  const int kv_head = unit / packs;
-  const int head0 = kv_head * P.group + (unit - kv_head * packs) * P.pack;
-  // keys that a token sees: the first `seen(tok)` of its sequence
-  auto seen = [&](int tok) { return P.causal ? max(0, min(len_k, tok + (len_k - len_q) + 1)) : len_k; };
-  const int tiles = (seen(min(tok0 + per_cta, len_q) - 1) + kPrTile - 1) / kPrTile;
-  const int cut = seen(tok0) / kPrTile;                      // tiles from here on are masked for some row
-  const bool two = tok0 + per_tile < len_q;                  // the second query tile has rows
-
-  // this thread's row
-  const int w = warp >> 2;                                   // softmax warps: query tile
-  const int r = threadIdx.x & 127;
-  const int tok = tok0 + w * per_tile + r / P.pack;
-  const bool row_ok = warp < 8 && tok < len_q;
-  const size_t out_row = (size_t)row0 + (size_t)tok;
-  const int head = head0 + r % P.pack;
-
-  if (tiles == 0) {                                          // no row of this CTA sees a key
-    if (row_ok) {
-      uint4* o = reinterpret_cast<uint4*>(P.O + out_row * P.ld_o + (size_t)head * HD);
-#pragma unroll
-      for (int i = 0; i < HD / 8; ++i) o[i] = make_uint4(0, 0, 0, 0);
-      if (P.lse) P.lse[out_row * P.n_q + head] = -INFINITY;
-    }
-    return;
-  }
-
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full(i), 1);
+      mbar_init(q_empty(i), 1);
       mbar_init(s_full(i), 1);
-      mbar_init(p_full(i), 4);
+      mbar_init(p_full(i, 0), 4);
+      mbar_init(p_full(i, 1), 4);
       mbar_init(o_full(i), 1);
+      mbar_init(o_empty(i), 4);
+      mbar_init(info_full(i), 1);
+      mbar_init(info_empty(i), 8 + 4 + 1 + 2);
+      mbar_init(stat_full(i), 4);
+      mbar_init(stat_empty(i), 4);
     }
+    mbar_init(answered, 1);
     for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 1); mbar_init(v_raw(i), 1); mbar_init(v_clean(i), 2); }
     misc[1] = 0;
-    misc[2] = 0;
     fence_mbar_init();
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
   }
-  if (warp == 9) {
+  if (warp == 13) {
     tmem_alloc(sbase + L::kMiscOff, 512);
     tmem_relinquish();
   }
@@ -222,173 +328,289 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-  const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 384};
+  auto s_col = [&](int i) { return tmem + 128u * i; };
+  auto o_col = [&](int i) { return tmem + 256u + 128u * i; };
+  // (parities of barriers that come in twos are kept as bits of one word: an array indexed at run time is local memory)
+  const int per_tile = kPrTile >> P.pack_log2;               // tokens
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax
     reg_inc<kPrSoftRegs>();
-    if (w == 0 || two) {
-      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t ts = s_col[w] + lanes, to = o_col[w] + lanes;
-      const int limit = tok < len_q ? seen(tok) : 0;
-      const float c = P.scale_log2;
+    const int w = warp >> 2, r = threadIdx.x & 127;          // query tile, row of it
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = s_col(w) + lanes, to = o_col(w) + lanes;
+    const float c = P.scale_log2;
+    uint32_t s_ph = 0, stat_ph = 0;
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 7)) break;
+      const TaskInfo* info = infos + (n & 1);
+      const int flags = info->flags, tiles = info->tiles, plain = min(info->cut, tiles);
+      // keys the row sees (not fewer in the rows behind it, those behind the sequence among them)
+      const int limit = P.causal ? max(0, min(info->len_k, info->tok0 + w * per_tile + (r >> P.pack_log2) + (info->len_k - info->len_q) + 1))
+                                 : info->len_k;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(info_empty(n & 1));
+      if (!(flags & 1)) break;
+      if (w == 1 && !(flags & 2)) continue;
       float m = -INFINITY;                                   // of S * c, when last renewed
-      uint64_t sum2 = 0;                                     // two partial sums of weights
-      bool ok = true;
-      for (int j = 0; j < tiles; ++j) {
-        if (!mbar_wait_warp(s_full(w), j & 1, abort_flag, P.status, 4)) { ok = false; break; }
+      uint64_t sum2[2] = {0, 0};                             // four partial sums of weights
+      // One tile of keys; MASKED: some row of the task does not see all of it.
+      auto tile = [&](int j, auto masked) -> bool {
+        constexpr bool MASKED = decltype(masked)::value;
+        if (!wait_long<true>(s_full(w), s_ph, abort_flag, P.status, 4)) return false;
+        s_ph ^= 1u;
         tc_fence_after();
         float x[128];
 #pragma unroll
         for (int b = 0; b < 4; ++b) tmem_ld_32x32(ts + b * 32, reinterpret_cast<uint32_t(&)[32]>(x[b * 32]));
-        const bool masked = j >= cut;
-        if (masked) {
-          const int n = limit - j * kPrTile;                 // columns that count
+        int most = 128;                                      // columns that count in the warp's last row
+        if (MASKED) {
+          const int n = limit - j * kPrTile, least = __shfl_sync(0xffffffffu, n, 0);
+          most = __shfl_sync(0xffffffffu, n, 31);
 #pragma unroll
-          for (int i = 0; i < 128; ++i) x[i] = i < n ? x[i] : -INFINITY;
+          for (int b = 0; b < 4; ++b)
+            if (least < b * 32 + 32) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[b * 32 + i] = b * 32 + i < n ? x[b * 32 + i] : -INFINITY;
+            }
         }
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < 128; i += 8)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = max3_nan(top[k], x[i + k], x[i + 4 + k]);
-        const float now = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * c;     // c > 0
-        const bool renew = now > m + 8.0f || m == -INFINITY || now != now;      // (a NaN takes the whole row)
+          for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], x[i + k]), x[i + 4 + k]);
+        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;     // c > 0; a NaN stays in its weight
+        const bool renew = now > m + 8.0f || m == -INFINITY;
         if (j > 0 && __any_sync(0xffffffffu, renew && now > m)) {
           // (the P V before is done: the S just read was issued behind it)
           const float f = renew && now > m ? (m == -INFINITY ? 0.0f : pow2_unit(m - now)) : 1.0f;
-          float s0, s1;
-          unpack2(sum2, s0, s1);
-          sum2 = pack2(s0 * f, s1 * f);
+          sum2[0] = mul2(sum2[0], pack2(f, f));
+          sum2[1] = mul2(sum2[1], pack2(f, f));
 #pragma unroll 1
-          for (int b = 0; b < HD / 32; ++b) {
-            uint32_t v[32];
-            tmem_ld_32x32(to + b * 32, v);
+          for (int b = 0; b < HD / 8; ++b) {
+            uint32_t v[8];
+            tmem_ld_32x8(to + b * 8, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            tmem_st_32x32(to + b * 32, v);
+            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_st_32x8(to + b * 8, v);
           }
           tmem_wait_st();
         }
-        if (renew && !(now < m)) m = now;
+        if (renew) m = fmaxf(m, now);
         const float minus = m == -INFINITY ? 0.0f : -m;
         const uint64_t c2 = pack2(c, c), m2 = pack2(minus, minus);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          uint32_t pk[16];
+        for (int b = 0; b < 8; ++b) {                        // 16 keys: a step of P V
+          uint32_t pk[8];
+          if (MASKED && most <= b * 16) {                    // nobody sees these keys
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float u, v;
-            unpack2(fma2(pack2(x[b * 32 + 2 * i], x[b * 32 + 2 * i + 1]), c2, m2), u, v);
-            if ((i & 3) == 3 && !masked) {
-              pow2_poly(u, v);
-            } else {
+            for (int i = 0; i < 8; ++i) pk[i] = 0;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float u, v;
+              unpack2(fma2(pack2(x[b * 16 + 2 * i], x[b * 16 + 2 * i + 1]), c2, m2), u, v);
               u = pow2_unit(u);
               v = pow2_unit(v);
+              sum2[i & 1] = add2(sum2[i & 1], pack2(u, v));
+              pk[i] = f32x2_to_bf16x2_bits(u, v);
             }
-            sum2 = add2(sum2, pack2(u, v));
-            pk[i] = f32x2_to_bf16x2_bits(u, v);
           }
-          tmem_st_32x16(ts + b * 16, pk);
+          tmem_st_32x8(ts + b * 8, pk);
+          if (b == kPrEarly - 1 || b == 7) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full(w, b == 7));
+          }
         }
-        tmem_wait_st();
-        tc_fence_before();
+        return true;
+      };
+      for (int j = 0; ok && j < plain; ++j) ok = tile(j, std::false_type{});
+      for (int j = plain; ok && j < tiles; ++j) ok = tile(j, std::true_type{});
+      if (!ok) break;
+      // what the end of the task needs
+      ok = wait_long<true>(stat_empty(w), stat_ph ^ 1u, abort_flag, P.status, 5);
+      stat_ph ^= 1u;
+      float s0, s1;
+      unpack2(add2(sum2[0], sum2[1]), s0, s1);
+      if (ok) stats[w * kPrTile + r] = make_float2(m, s0 + s1);
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(stat_full(w));
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------ the end of a task
+    reg_dec<kPrEndRegs>();
+    const int r = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    uint32_t ph = 0, o_ph = 0;
+    const int pack_mask = (1 << P.pack_log2) - 1;
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 9)) break;
+      const volatile TaskInfo* info = infos + (n & 1);
+      if (!(info->flags & 1)) break;
+      const int tiles = info->tiles, len_q = info->len_q, row0 = info->row0, head0 = info->head0;
+#pragma unroll 1
+      for (int w = 0; w < ((info->flags & 2) ? 2 : 1); ++w) {
+        ok = wait_long<true>(stat_full(w), ph >> w & 1u, abort_flag, P.status, 9);
+        if (!ok) break;
+        ph ^= 1u << w;
+        const float2 ms = stats[w * kPrTile + r];
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(w));
-      }
-      if (ok && mbar_wait_warp(o_full(w), (tiles - 1) & 1, abort_flag, P.status, 5)) {
-        tc_fence_after();
-        float s0, s1;
-        unpack2(sum2, s0, s1);
-        const float sum = s0 + s1;
+        if (lane == 0) mbar_arrive(stat_empty(w));
+        const float sum = ms.y;                              // (no tiles: 0)
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-        const bool odd = *odd_values != 0;
-        __nv_bfloat16* o = P.O + out_row * P.ld_o + (size_t)head * HD;
+        const int tok0 = info->tok0 + w * per_tile;
+        const bool row_ok = tok0 + (r >> P.pack_log2) < len_q;
+        bool odd = false;
+        if (tiles > 0) {
+          ok = wait_long<true>(o_full(w), o_ph >> w & 1u, abort_flag, P.status, 9);
+          if (!ok) break;
+          o_ph ^= 1u << w;
+          tc_fence_after();
+          odd = info->odd != 0;
+        }
 #pragma unroll 1
         for (int b = 0; b < HD / 32; ++b) {
           uint32_t v[32];
-          tmem_ld_32x32(to + b * 32, v);
-          if (row_ok) {
-            if (odd) {
-              // what the cut tiles' zeros stand for: a value that is not finite outweighs every finite sum
-              for (int k = cut * kPrTile; k < limit; ++k) {
-                const __nv_bfloat16* val = P.V + (size_t)(key0 + k) * P.ld_v + (size_t)kv_head * HD + b * 32;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const float z = __bfloat162float(val[i]);
-                  if (!(fabsf(z) < INFINITY)) v[i] = __float_as_uint(__uint_as_float(v[i]) + z);
-                }
-              }
+          if (tiles > 0) {
+            tmem_ld_32x32(o_col(w) + lanes + b * 32, v);
+            if (b == HD / 32 - 1) {                          // the next task's sums may begin
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(o_empty(w));
             }
-            uint32_t y[16];
+          }
+          uint4 y[4];                                        // 32 elements of this lane's row
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              y[i] = f32x2_to_bf16x2_bits(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+          for (int i = 0; i < 4; ++i) {
+            uint32_t z[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<uint4*>(o + b * 32 + i * 8) = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+            for (int k = 0; k < 4; ++k)
+              z[k] = tiles > 0 ? f32x2_to_bf16x2_bits(__uint_as_float(v[8 * i + 2 * k]) * inv, __uint_as_float(v[8 * i + 2 * k + 1]) * inv) : 0u;
+            y[i] = make_uint4(z[0], z[1], z[2], z[3]);
+          }
+          // Four lanes swap their quarters, so that a store covers 64 bytes of eight rows; with a row a lane every store met 32
+          // lines (16 stores a lane and task: 4 000 cycles).
+          transpose4(y, lane);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int from = (r & ~3) + i, tok = tok0 + (from >> P.pack_log2);        // whose row
+            if (tok < len_q)
+              *reinterpret_cast<uint4*>(P.O + (size_t)(row0 + tok) * P.ld_o + (size_t)(head0 + (from & pack_mask)) * HD + b * 32 +
+                                        (lane & 3) * 8) = y[i];
           }
         }
+        if (odd) {
+          __syncwarp();                                      // (the row was written by four lanes)
+          const int limit = P.causal ? min(info->len_k, tok0 + (r >> P.pack_log2) + (info->len_k - len_q) + 1) : info->len_k;
+          if (row_ok)
+            add_odd_values(P.V + (size_t)info->key0 * P.ld_v + (size_t)info->kv_head * HD, P.ld_v, HD, info->cut * kPrTile, limit,
+                           P.O + (size_t)(row0 + tok0 + (r >> P.pack_log2)) * P.ld_o + (size_t)(head0 + (r & pack_mask)) * HD);
+        }
         if (row_ok && P.lse)
-          P.lse[out_row * P.n_q + head] =
-              sum > 0.0f || sum != sum ? m * 0.69314718055994531f + logf(sum) : -INFINITY;
+          P.lse[(size_t)(row0 + tok0 + (r >> P.pack_log2)) * P.n_q + head0 + (r & pack_mask)] =
+              sum > 0.0f || sum != sum ? ms.x * 0.69314718055994531f + logf(sum) : -INFINITY;
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(info_empty(n & 1));         // (at the end: `odd` comes late)
     }
   } else {
     reg_dec<kPrAuxRegs>();
-    if (warp == 8) {
-      // ---------------------------------------------------------------- TMA
-      if (elect_one()) {
-        int st = 0; uint32_t ph = 0, armed = 0, armed_par = 0;
-        bool ok = true;
-        auto queries = [&](int i) {
-          mbar_arrive_expect_tx(q_full(i), L::kMat);
-#pragma unroll
-          for (int h = 0; h < HD / 64; ++h)
-            tma_load_3d(sbase + i * L::kMat + h * L::kHalf, &tmQ, q_full(i), h * 64, head0, row0 + tok0 + i * per_tile);
-        };
-        uint32_t raw_par = 0;                                 // per stage: parity of the next phase of v_raw
-        auto fetch = [&](const CUtensorMap* tm, int j, bool clean) {
-          if (!mbar_wait(kv_empty(st), ph ^ 1u, abort_flag, P.status, 1)) return false;
-          // values to be cleaned arrive on a barrier of their own, whose every phase the cleaning warps see
-          const uint32_t bar = clean ? v_raw(st) : kv_full(st);
+    if (warp == 12) {
+      // ---------------------------------------------------------------- tasks and TMA
+      const uint32_t answer = sbase + L::kMiscOff + 16;
+      uint32_t kv_ph = 0, armed = 0, armed_par = 0, raw_par = 0, asked = 0;
+      uint32_t q_ph = 0;
+      int st = 0;
+      bool ok = true;
+      int bid = blockIdx.x;
+      const TaskOrder order = task_order(P, lane);
+      auto fetch = [&](const CUtensorMap* tm, int kv_head, int row, bool clean) -> bool {
+        if (!wait_long<true>(kv_empty(st), kv_ph ^ 1u, abort_flag, P.status, 1)) return false;
+        // values to be cleaned arrive on a barrier of their own, whose every phase the cleaning warps see
+        const uint32_t bar = clean ? v_raw(st) : kv_full(st);
+        if (lane == 0) {
           if (clean) mbar_arrive(kv_full(st));
           mbar_arrive_expect_tx(bar, L::kMat);
 #pragma unroll
           for (int h = 0; h < HD / 64; ++h)
-            tma_load_2d(sbase + L::kKvOff + st * L::kMat + h * L::kHalf, tm, bar, kv_head * HD + h * 64, key0 + j * kPrTile);
-          const int slot = clean ? ST + st : st;
-          armed |= 1u << slot;
-          armed_par = (armed_par & ~(1u << slot)) | ((clean ? raw_par >> st & 1u : ph) << slot);
-          if (clean) raw_par ^= 1u << st;
-          if (++st == ST) { st = 0; ph ^= 1u; }
-          return true;
-        };
-        queries(0);
-        ok = fetch(&tmK, 0, false);
-        if (two) queries(1);
-        ok = ok && fetch(&tmV, 0, cut == 0);
-        for (int j = 1; ok && j < tiles; ++j) ok = fetch(&tmK, j, false) && fetch(&tmV, j, j >= cut);
-        if (!ok) {
-          const uint64_t t0 = globaltimer_ns();
-          for (int i = 0; i < 2 * ST; ++i)
-            if (armed & (1u << i))
-              while (!mbar_try_wait(i < ST ? kv_full(i) : v_raw(i - ST), (armed_par >> i) & 1u) &&
-                     globaltimer_ns() - t0 < 2000000ull) {}
+            tma_load_2d(sbase + L::kKvOff + st * L::kMat + h * L::kHalf, tm, bar, kv_head * HD + h * 64, row);
         }
+        const int slot = clean ? ST + st : st;
+        armed |= 1u << slot;
+        armed_par = (armed_par & ~(1u << slot)) | ((clean ? raw_par >> st & 1u : kv_ph) << slot);
+        if (clean) raw_par ^= 1u << st;
+        if (++st == ST) { st = 0; kv_ph ^= 1u; }
+        return true;
+      };
+      for (int n = 0; ok;) {
+        // the task of block `bid`, if it is one
+        TaskInfo ti = {};
+        const bool found = bid >= 0 && find_prompt_task(P, order, bid, lane, ti);
+        if (found || bid < 0) {
+          if (!wait_long<true>(info_empty(n & 1), ((n >> 1) & 1) ^ 1u, abort_flag, P.status, 1)) { ok = false; break; }
+          if (lane == 0) {
+            infos[n & 1] = ti;
+            mbar_arrive(info_full(n & 1));
+          }
+          ++n;
+          if (bid < 0) break;
+          if (ti.tiles > 0) {
+            auto queries = [&](int i) -> bool {
+              if (!wait_long<true>(q_empty(i), (q_ph >> i & 1u) ^ 1u, abort_flag, P.status, 1)) return false;
+              q_ph ^= 1u << i;
+              if (lane == 0) {
+                mbar_arrive_expect_tx(q_full(i), L::kMat);
+#pragma unroll
+                for (int h = 0; h < HD / 64; ++h)
+                  tma_load_3d(sbase + i * L::kMat + h * L::kHalf, &tmQ, q_full(i), h * 64, ti.head0, ti.row0 + ti.tok0 + i * per_tile);
+              }
+              return true;
+            };
+            ok = queries(0) && fetch(&tmK, ti.kv_head, ti.key0, false);
+            if (ti.flags & 2) ok = ok && queries(1);
+            ok = ok && fetch(&tmV, ti.kv_head, ti.key0, ti.cut == 0);
+            for (int j = 1; ok && j < ti.tiles; ++j)
+              ok = fetch(&tmK, ti.kv_head, ti.key0 + j * kPrTile, false) &&
+                   fetch(&tmV, ti.kv_head, ti.key0 + j * kPrTile, j >= ti.cut);
+            if (!ok) break;
+          }
+        }
+        // a block that was not started yet, or none (not asked for earlier: a task that waits here could be another CTA's)
+        if (lane == 0) {
+          mbar_arrive_expect_tx(answered, 16);
+          ask_for_a_block(answer, answered);
+        }
+        if (!wait_long<true>(answered, asked & 1u, abort_flag, P.status, 8)) { ok = false; break; }
+        ++asked;
+        bid = block_of_answer(answer);
+        fence_proxy_async_smem();                            // (the answer is read before the next one is written)
+        __syncwarp();
       }
-    } else if (warp == 9) {
+      if (!ok) {
+        // copies in flight (queries among them: their barrier's last phase) before this CTA's shared memory goes away
+        const uint64_t t0 = globaltimer_ns();
+        for (int i = 0; i < 2 * ST; ++i)
+          if (armed & (1u << i))
+            while (!mbar_try_wait(i < ST ? kv_full(i) : v_raw(i - ST), (armed_par >> i) & 1u) && globaltimer_ns() - t0 < 2000000ull) {}
+        for (int i = 0; i < 2; ++i)
+          while (!mbar_try_wait(q_full(i), (q_ph >> i & 1u) ^ 1u) && globaltimer_ns() - t0 < 2000000ull) {}
+      }
+    } else if (warp == 13) {
       // ---------------------------------------------------------------- tensor core
       if (elect_one()) {
         constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128, false), idesc_o = umma_idesc_bf16(128, HD, true);
-        const int nw = two ? 2 : 1;
-        int st = 0; uint32_t ph = 0;                          // ring: keys 0, values 0, keys 1, ...
+        int st = 0; uint32_t ph = 0;                          // ring: keys 0, values 0, keys 1, ... of all tasks
         int k_st = 0, v_st = 0;
         uint32_t clean_par = 0;                               // per stage: parity of the next phase of v_clean
+        uint32_t q_ph = 0, o_ph = 0, p_ph = 0;
         bool ok = true;
         auto next = [&](int& mine) {
           mine = st;
-          const bool got = mbar_wait(kv_full(st), ph, abort_flag, P.status, 2);
+          const bool got = wait_long<false>(kv_full(st), ph, abort_flag, P.status, 2);
           if (++st == ST) { st = 0; ph ^= 1u; }
           return got;
         };
@@ -398,36 +620,57 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           for (int h = 0; h < HD / 64; ++h) {
             const uint64_t ad = umma_desc_kmajor_sw128(a + h * L::kHalf), bd = umma_desc_kmajor_sw128(b + h * L::kHalf);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(s_col[i], ad + 2u * k, bd + 2u * k, idesc_s, (h | k) != 0);
+            for (int k = 0; k < 4; ++k) umma_bf16(s_col(i), ad + 2u * k, bd + 2u * k, idesc_s, (h | k) != 0);
           }
           umma_commit(s_full(i));
         };
-        ok = next(k_st);
-        for (int i = 0; ok && i < nw; ++i) {
-          ok = mbar_wait(q_full(i), 0, abort_flag, P.status, 2);
-          if (ok) { tc_fence_after(); scores(i); }
-        }
-        if (ok) umma_commit(kv_empty(k_st));
-        for (int j = 0; ok && j < tiles; ++j) {
-          ok = next(v_st);
-          if (ok && j >= cut) {
-            ok = mbar_wait(v_clean(v_st), (clean_par >> v_st) & 1u, abort_flag, P.status, 3);
-            clean_par ^= 1u << v_st;
-          }
-          if (ok && j + 1 < tiles) ok = next(k_st);
+        for (int n = 0; ok; ++n) {
+          if (!wait_long<false>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 2)) break;
+          const volatile TaskInfo* info = infos + (n & 1);
+          const int flags = info->flags, tiles = info->tiles, cut = info->cut;
+          mbar_arrive(info_empty(n & 1));
+          if (!(flags & 1)) break;
+          if (tiles == 0) continue;
+          const int nw = (flags & 2) ? 2 : 1;
+          ok = next(k_st);
           for (int i = 0; ok && i < nw; ++i) {
-            ok = mbar_wait(p_full(i), j & 1, abort_flag, P.status, 3);
+            ok = wait_long<false>(q_full(i), q_ph >> i & 1u, abort_flag, P.status, 2);
+            q_ph ^= 1u << i;
             if (!ok) break;
             tc_fence_after();
-            const uint64_t bd = umma_desc_mnmajor_sw128(sbase + L::kKvOff + v_st * L::kMat, L::kHalf);
-#pragma unroll
-            for (int k = 0; k < kPrTile / 16; ++k)
-              umma_bf16_ts(o_col[i], s_col[i] + 8u * k, bd + 128u * k, idesc_o, (j | k) != 0);
-            umma_commit(o_full(i));
-            if (i == nw - 1) umma_commit(kv_empty(v_st));
-            if (j + 1 < tiles) {
-              scores(i);
-              if (i == nw - 1) umma_commit(kv_empty(k_st));
+            scores(i);
+            if (tiles == 1) umma_commit(q_empty(i));
+          }
+          if (ok) umma_commit(kv_empty(k_st));
+          for (int j = 0; ok && j < tiles; ++j) {
+            ok = next(v_st);
+            if (ok && j >= cut) {
+              ok = wait_long<false>(v_clean(v_st), (clean_par >> v_st) & 1u, abort_flag, P.status, 3);
+              clean_par ^= 1u << v_st;
+            }
+            for (int i = 0; ok && i < nw; ++i) {
+              if (j == 0) {                                   // the sums of the task before were read
+                ok = wait_long<false>(o_empty(i), (o_ph >> i & 1u) ^ 1u, abort_flag, P.status, 3);
+                o_ph ^= 1u << i;
+              }
+              const uint64_t bd = umma_desc_mnmajor_sw128(sbase + L::kKvOff + v_st * L::kMat, L::kHalf);
+              for (int part = 0; ok && part < 2; ++part) {
+                ok = wait_long<false>(p_full(i, part), p_ph >> i & 1u, abort_flag, P.status, 3);
+                if (!ok) break;
+                tc_fence_after();
+                for (int k = part ? kPrEarly : 0; k < (part ? kPrTile / 16 : kPrEarly); ++k)
+                  umma_bf16_ts(o_col(i), s_col(i) + 8u * k, bd + 128u * k, idesc_o, (j | k) != 0);
+              }
+              if (!ok) break;
+              p_ph ^= 1u << i;
+              if (j + 1 == tiles) umma_commit(o_full(i));
+              if (i == nw - 1) umma_commit(kv_empty(v_st));
+              if (j + 1 < tiles) {
+                if (i == 0 && !(ok = next(k_st))) break;
+                scores(i);
+                if (j + 2 == tiles) umma_commit(q_empty(i));
+                if (i == nw - 1) umma_commit(kv_empty(k_st));
+              }
             }
           }
         }
@@ -435,36 +678,59 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else {
       // ---------------------------------------------------------------- values of the cut tiles
       uint32_t raw_par = 0;
-      for (int j = cut; j < tiles; ++j) {
-        const int st = (2 * j + 1) % ST;                      // place in the ring
-        if (!mbar_wait_warp(v_raw(st), (raw_par >> st) & 1u, abort_flag, P.status, 6)) break;
-        raw_par ^= 1u << st;
-        uint8_t* v = smem + L::kKvOff + st * L::kMat;
-        bool odd = false;
-        for (int i = (warp - 10) * 32 + lane; i < L::kMat / 16; i += 64) {
-          const int row = (i >> 3) & 127;                     // 128-byte rows, 128 of them for each 64 columns
-          uint4* p = reinterpret_cast<uint4*>(v + (size_t)i * 16);
-          uint4 x = *p;
-          if (j * kPrTile + row >= len_k) {
-            *p = make_uint4(0, 0, 0, 0);
-          } else {
-            uint32_t y[4] = {x.x, x.y, x.z, x.w};
-            uint32_t hit = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              // the exponent's bits carry into the sign's when they are all ones
-              const uint32_t e = ((y[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-              if (e & 0x8000u) y[k] &= 0xFFFF0000u;
-              if (e & 0x80000000u) y[k] &= 0x0000FFFFu;
-              hit |= e;
-            }
-            if (hit) { *p = make_uint4(y[0], y[1], y[2], y[3]); odd = true; }
+      int first = 1;                                          // place in the ring of the task's first values
+      for (int n = 0;; ++n) {
+        if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 6)) break;
+        TaskInfo* info = infos + (n & 1);
+        const int flags = info->flags, tiles = info->tiles, cut = info->cut, len_k = info->len_k;
+        bool ok = true;
+        for (int j = cut; ok && j < tiles; ++j) {
+          const int st = (first + 2 * j) % ST;
+          ok = wait_long<true>(v_raw(st), (raw_par >> st) & 1u, abort_flag, P.status, 6);
+          if (!ok) break;
+          raw_par ^= 1u << st;
+          // this thread's 16-byte pieces: every 64th; 128-byte rows, 128 of them for each 64 columns
+          uint4* v = reinterpret_cast<uint4*>(smem + L::kKvOff + st * L::kMat) + (warp - 14) * 32 + lane;
+          constexpr int N = L::kMat / 16 / 64;
+          const int rows = len_k - j * kPrTile, row = ((warp - 14) * 32 + lane) >> 3;     // piece i: row + 8 i of its half
+          if (rows < kPrTile) {
+#pragma unroll 4
+            for (int i = 0; i < N; ++i)
+              if (((row + 8 * i) & 127) >= rows) v[64 * i] = make_uint4(0, 0, 0, 0);
           }
+          // zero times a value is NaN where the value is not finite
+          __nv_bfloat162 sum = __floats2bfloat162_rn(0.0f, 0.0f);
+          const __nv_bfloat162 zero = sum;
+#pragma unroll 1
+          for (int i = 0; i < N; i += 8) {
+            uint4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = v[64 * (i + k)];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t y[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&y[e]), zero, sum);
+            }
+          }
+          if (__hisnan(sum.x) || __hisnan(sum.y)) {
+            for (int i = 0; i < N; ++i) {
+              uint32_t* x = reinterpret_cast<uint32_t*>(v + 64 * i);
+              for (int e = 0; e < 4; ++e) {
+                if ((x[e] & 0x7F80u) == 0x7F80u) x[e] &= 0xFFFF0000u;
+                if ((x[e] & 0x7F800000u) == 0x7F800000u) x[e] &= 0x0000FFFFu;
+              }
+            }
+            *reinterpret_cast<volatile int*>(&info->odd) = 1;
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_clean(st));
         }
-        if (odd) *odd_values = 1;
-        fence_proxy_async_smem();
+        first = (first + 2 * tiles) % ST;
         __syncwarp();
-        if (lane == 0) mbar_arrive(v_clean(st));
+        if (lane == 0) mbar_arrive(info_empty(n & 1));
+        if (!ok || !(flags & 1)) break;
       }
     }
   }
@@ -472,7 +738,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   // ---- teardown
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 13) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -511,10 +777,10 @@ static int launch_prompt(cudaStream_t st, const void* Q, int ld_q, const void* K
   static PerDeviceInt attr_set;
   if (!ensure_smem_attr(attr_set, kern, L::kAlloc)) return FPT_ERR_CUDA;
   CUtensorMap tmQ, tmK, tmV;
-  if (!make_query_map(&tmQ, Q, HD, P.n_q, P.M_q, ld_q, P.pack) || !make_rows_map(&tmK, K, P.n_kv * HD, P.M_k, ld_k) ||
+  if (!make_query_map(&tmQ, Q, HD, P.n_q, P.M_q, ld_q, 1 << P.pack_log2) || !make_rows_map(&tmK, K, P.n_kv * HD, P.M_k, ld_k) ||
       !make_rows_map(&tmV, V, P.n_kv * HD, P.M_k, P.ld_v))
     return FPT_ERR_CUDA;
-  const int64_t tasks = (int64_t)P.M_q / (2 * kPrTile / P.pack) + P.n_seqs;
+  const int64_t tasks = (int64_t)P.M_q / (2 * kPrTile >> P.pack_log2) + P.n_seqs;
   if (tasks * P.units > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   P.n_tasks = (int)tasks;
   return launch_kernel(kern, dim3((unsigned)(tasks * P.units)), dim3(kPrThreads), L::kAlloc, st, true, tmQ, tmK, tmV, P) ==
@@ -549,9 +815,8 @@ extern "C" int fpt_attn_prompt(void* stream, const void* Q, int ld_q, int M_q, c
   P.lse = lse;
   P.status = reinterpret_cast<uint32_t*>(workspace);
   P.ld_v = ld_v; P.ld_o = ld_o; P.M_q = M_q; P.M_k = M_k; P.n_q = n_q; P.n_kv = n_kv; P.group = n_q / n_kv;
-  P.pack = 1;
-  while (P.pack < 16 && P.group % (2 * P.pack) == 0) P.pack *= 2;
-  P.units = n_q / P.pack;
+  while (P.pack_log2 < 4 && (P.group >> P.pack_log2) % 2 == 0) ++P.pack_log2;
+  P.units = n_q >> P.pack_log2;
   P.n_seqs = n_seqs; P.causal = causal != 0;
   P.scale_log2 = scale * 1.4426950408889634f;
   return head_dim == 128 ? launch_prompt<128>((cudaStream_t)stream, Q, ld_q, K, ld_k, V, P)
