@@ -47,18 +47,21 @@ class _KVCacheStruct(ctypes.Structure):
 class KVCache:
     """A paged 8-bit cache (see `fpt_kv_cache`): codes int8 [n_pages, n_kv, page, head_dim], scales f32 [n_pages, n_kv],
     page table int32 [n_seqs, max_pages], all contiguous on one device."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_kv", "head_dim", "struct", "ref")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "struct", "ref")
 
     def __init__(self, k, v, k_scale, v_scale, pages):
-        n_pages, n_kv, page, hd = k.shape
-        for t, dtype, shape in ((k, torch.int8, k.shape), (v, torch.int8, k.shape), (k_scale, torch.float32, (n_pages, n_kv)),
-                                (v_scale, torch.float32, (n_pages, n_kv)), (pages, torch.int32, pages.shape)):
-            if t.dtype is not dtype or t.shape != shape or t.dim() < 2 or not t.is_contiguous():
-                raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table are wanted")
+        shape = k.shape
+        n_pages, n_kv, page, hd = shape
+        if not (k.dtype is torch.int8 and v.dtype is torch.int8 and k_scale.dtype is torch.float32 and
+                v_scale.dtype is torch.float32 and pages.dtype is torch.int32 and v.shape == shape and
+                k_scale.shape == shape[:2] and v_scale.shape == shape[:2] and pages.dim() == 2 and k.is_contiguous() and
+                v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous() and pages.is_contiguous()):
+            raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table are wanted")
         self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
         self.n_kv, self.head_dim = n_kv, hd
+        self.n_seqs, max_pages = pages.shape
         self.struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages.data_ptr(),
-                                     n_pages, n_kv, page, hd, pages.shape[1])
+                                     n_pages, n_kv, page, hd, max_pages)
         self.ref = ctypes.byref(self.struct)
 
     @classmethod
@@ -66,7 +69,7 @@ class KVCache:
         """Stands for no storage: fpt_rope_append then only rotates."""
         c = cls.__new__(cls)
         c.k = c.v = c.k_scale = c.v_scale = c.pages = None
-        c.n_kv, c.head_dim = n_kv, head_dim
+        c.n_seqs, c.n_kv, c.head_dim = 0, n_kv, head_dim
         c.struct = _KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0)
         c.ref = ctypes.byref(c.struct)
         return c
@@ -349,104 +352,128 @@ def new_kv_cache(n_pages, n_kv, page, head_dim, pages, device="cuda"):
     return KVCache(k, v, ks, vs, pages)
 
 
-# What the attention calls ask of a tensor (their rows may be places in a wider buffer).
+# What the attention calls ask of a tensor (their rows may be places in a wider buffer), and how they allocate: a decode step's
+# kernel takes about as long as these lines, so an attribute is read once, and what resembles an input is made from it
+# (torch.empty_like and new_empty cost half of torch.empty).
+def _bad(where):
+    return FptError(ERR_BAD_ARG, where)
+
+
 def _rows(t, where):
     """Leading dimension of a bf16 [rows, columns] tensor whose rows are contiguous."""
-    if t.dtype is not torch.bfloat16 or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
-        raise FptError(ERR_BAD_ARG, where)
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    strides = t.stride()
+    if t.dtype is not torch.bfloat16 or len(strides) != 2 or strides[1] != 1:
+        raise _bad(where)
+    ld, (rows, cols) = strides[0], t.shape
+    return ld if rows > 1 or ld >= cols else cols
 
 
 def _i32(t, n, where):
     """Address of an int32 [n] tensor."""
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise FptError(ERR_BAD_ARG, where)
+    if t.dtype is not torch.int32 or t.shape != (n,) or (n > 1 and t.stride() != (1,)):
+        raise _bad(where)
     return t.data_ptr()
+
+
+def _like(t):
+    return torch.empty_like(t) if _allocator is None else _empty(t.shape, t.dtype, t.device)
+
+
+def _new(t, shape, dtype):
+    return t.new_empty(shape, dtype=dtype) if _allocator is None else _empty(shape, dtype, t.device)
 
 
 def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, want_k=False, Q=None, K=None, ws=None):
     """QKV [M, (n_q + 2 n_kv) head_dim] bf16, rope f32 [n_pos, rot_dim / 2, 2], ctx int32 [n_seqs], cu_new int32 [n_seqs + 1]
     (None: row s is sequence s's token) -> (rotated queries bf16 [M, n_q head_dim], rotated keys [M, n_kv head_dim] or None).
     Keys and values go to the cache (KVCache.heads(n_kv, head_dim): nowhere)."""
+    where = "fpt_rope_append"
     M, cols = QKV.shape
-    ld, hd, n_kv = _rows(QKV, "fpt_rope_append"), cache.head_dim, cache.n_kv
-    if (rope.dtype is not torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or
-            cols < (n_q + 2 * n_kv) * hd or (cache.pages is not None and cache.pages.shape[0] < ctx.shape[0])):
-        raise FptError(ERR_BAD_ARG, "fpt_rope_append")
-    n = ctx.shape[0]
+    hd, n_kv, n = cache.head_dim, cache.n_kv, ctx.shape[0]
+    n_pos, pairs, two = rope.shape
+    if (rope.dtype is not torch.float32 or two != 2 or not rope.is_contiguous() or cols < (n_q + 2 * n_kv) * hd or
+            (cache.pages is not None and cache.n_seqs < n)):
+        raise _bad(where)
     if Q is None:
-        Q = _empty((M, n_q * hd), dtype=torch.bfloat16, device=QKV.device)
-    if K is None and want_k:
-        K = _empty((M, n_kv * hd), dtype=torch.bfloat16, device=QKV.device)
+        Q = _new(QKV, (M, n_q * hd), torch.bfloat16)
+    elif Q.shape != (M, n_q * hd):
+        raise _bad(where)
+    if K is None:
+        if want_k:
+            K = _new(QKV, (M, n_kv * hd), torch.bfloat16)
+    elif K.shape != (M, n_kv * hd):
+        raise _bad(where)
     if ws is None:
         ws = new_workspace(OP_ATTN, 1, 1, 1, QKV.device)
-    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, ld, n_q, rope.data_ptr(), rope.shape[0], 2 * rope.shape[1], layout,
-                                 None if cu_new is None else _i32(cu_new, n + 1, "fpt_rope_append"),
-                                 _i32(ctx, n, "fpt_rope_append"), n, cache.ref, Q.data_ptr(), _rows(Q, "fpt_rope_append"),
-                                 _ptr(K), 0 if K is None else _rows(K, "fpt_rope_append"), ws.data_ptr(), ws.numel()),
-           "fpt_rope_append")
+    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, _rows(QKV, where), n_q, rope.data_ptr(), n_pos, 2 * pairs, layout,
+                                 None if cu_new is None else _i32(cu_new, n + 1, where), _i32(ctx, n, where), n, cache.ref,
+                                 Q.data_ptr(), _rows(Q, where), None if K is None else K.data_ptr(),
+                                 0 if K is None else _rows(K, where), ws.data_ptr(), ws.numel()), where)
     return Q, K
 
 
 def fpt_kv_gather(cache, cu_out, M, first=None, K=None, V=None, ws=None):
     """Cached tokens first[s] ... of every sequence in bf16 -> (K, V) [M, n_kv head_dim], packed by cu_out int32 [n_seqs + 1]."""
-    n, cols = cu_out.shape[0] - 1, cache.n_kv * cache.head_dim
-    if cache.pages is None or cache.pages.shape[0] < n:
-        raise FptError(ERR_BAD_ARG, "fpt_kv_gather")
+    where = "fpt_kv_gather"
+    n, shape = cu_out.shape[0] - 1, (M, cache.n_kv * cache.head_dim)
+    if cache.pages is None or cache.n_seqs < n:
+        raise _bad(where)
     if K is None:
-        K = _empty((M, cols), dtype=torch.bfloat16, device=cu_out.device)
+        K = _new(cu_out, shape, torch.bfloat16)
     if V is None:
-        V = _empty((M, cols), dtype=torch.bfloat16, device=cu_out.device)
+        V = _like(K) if K.is_contiguous() else _new(cu_out, shape, torch.bfloat16)
     if ws is None:
         ws = new_workspace(OP_ATTN, 1, 1, 1, cu_out.device)
-    ld = _rows(K, "fpt_kv_gather")
-    if _rows(V, "fpt_kv_gather") != ld or K.shape[0] < M or V.shape[0] < M:
-        raise FptError(ERR_BAD_ARG, "fpt_kv_gather")
-    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, "fpt_kv_gather"),
-                               _i32(cu_out, n + 1, "fpt_kv_gather"), n, M, K.data_ptr(), V.data_ptr(), ld, ws.data_ptr(), ws.numel()),
-           "fpt_kv_gather")
+    ld = _rows(K, where)
+    if _rows(V, where) != ld or K.shape != shape or V.shape != shape:
+        raise _bad(where)
+    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, where), _i32(cu_out, n + 1, where),
+                               n, M, K.data_ptr(), V.data_ptr(), ld, ws.data_ptr(), ws.numel()), where)
     return K, V
 
 
 def fpt_attn_decode(Q, cache, kv_len, scale=None, want_lse=False, O=None, ws=None):
     """Q [n_seqs, n_q head_dim] bf16, kv_len int32 [n_seqs] -> (O like Q, lse f32 [n_seqs, n_q] or None)."""
-    n, cols = Q.shape
+    where = "fpt_attn_decode"
+    n, cols = shape = Q.shape
     hd = cache.head_dim
-    if cache.pages is None or cache.pages.shape[0] < n or cols % hd:
-        raise FptError(ERR_BAD_ARG, "fpt_attn_decode")
+    n_q = cols // hd
+    if cache.n_seqs < n or cols != n_q * hd:
+        raise _bad(where)
     if O is None:
-        O = _empty((n, cols), dtype=torch.bfloat16, device=Q.device)
-    elif O.shape != Q.shape:
-        raise FptError(ERR_BAD_ARG, "fpt_attn_decode")
-    lse = _empty((n, cols // hd), dtype=torch.float32, device=Q.device) if want_lse else None
+        O = _like(Q)
+    elif O.shape != shape:
+        raise _bad(where)
+    lse = _new(Q, (n, n_q), torch.float32) if want_lse else None
     if ws is None:
         ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
-    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, "fpt_attn_decode"), cols // hd, cache.ref,
-                                 _i32(kv_len, n, "fpt_attn_decode"), n, hd ** -0.5 if scale is None else scale, O.data_ptr(),
-                                 _rows(O, "fpt_attn_decode"), _ptr(lse), ws.data_ptr(), ws.numel()), "fpt_attn_decode")
+    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, where), n_q, cache.ref, _i32(kv_len, n, where), n,
+                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, where),
+                                 None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel()), where)
     return O, lse
 
 
 def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None, want_lse=False, O=None, ws=None):
     """Q [M_q, n_q head_dim], K and V [M_k, n_kv head_dim] bf16 (places in wider buffers will do), packed by cu_q, cu_k int32
     [n_seqs + 1] (cu_k None: cu_q) -> (O like Q, lse f32 [M_q, n_q] or None)."""
-    Mq, cols = Q.shape
+    where = "fpt_attn_prompt"
+    Mq, cols = shape = Q.shape
+    Mk, cols_k = K.shape
     hd, n = cols // n_q, cu_q.shape[0] - 1
-    if cols != n_q * hd or K.shape[1] != n_kv * hd or V.shape != K.shape:
-        raise FptError(ERR_BAD_ARG, "fpt_attn_prompt")
+    if cols != n_q * hd or cols_k != n_kv * hd or V.shape != K.shape:
+        raise _bad(where)
     if O is None:
-        O = _empty((Mq, cols), dtype=torch.bfloat16, device=Q.device)
-    elif O.shape != Q.shape:
-        raise FptError(ERR_BAD_ARG, "fpt_attn_prompt")
-    lse = _empty((Mq, n_q), dtype=torch.float32, device=Q.device) if want_lse else None
+        O = _like(Q)
+    elif O.shape != shape:
+        raise _bad(where)
+    lse = _new(Q, (Mq, n_q), torch.float32) if want_lse else None
     if ws is None:
         ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
-    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, "fpt_attn_prompt"), Mq, K.data_ptr(),
-                                 _rows(K, "fpt_attn_prompt"), V.data_ptr(), _rows(V, "fpt_attn_prompt"), K.shape[0], n_q, n_kv, hd,
-                                 _i32(cu_q, n + 1, "fpt_attn_prompt"),
-                                 None if cu_k is None else _i32(cu_k, n + 1, "fpt_attn_prompt"), n, int(bool(causal)),
-                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, "fpt_attn_prompt"), _ptr(lse),
-                                 ws.data_ptr(), ws.numel()), "fpt_attn_prompt")
+    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, where), Mq, K.data_ptr(), _rows(K, where), V.data_ptr(),
+                                 _rows(V, where), Mk, n_q, n_kv, hd, _i32(cu_q, n + 1, where),
+                                 None if cu_k is None else _i32(cu_k, n + 1, where), n, int(bool(causal)),
+                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, where),
+                                 None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel()), where)
     return O, lse
 
 

@@ -68,27 +68,26 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435e-38f ? __fdiv_rn(1.0f, s) : 0.0f; }
 
 // A launch over the pages (or blocks of `block` rows) that packed sequences touch, without their lengths on the host:
-// sequence s, rows cu[s] .. cu[s+1]-1, is given floor(cu[s+1] / block) - floor(cu[s] / block) + extra tasks, which
-// is at least the number of blocks of its rows (extra = 1: blocks count from its first row; 2: they count from any row), and
-// task `id` belongs to the last s whose tasks start at or before it.  All sequences are looked at side by side: one round of loads
-// where a binary search would wait for one load after the other.  Returns s or -1, the same in every thread, and the place among its tasks.
-__device__ __forceinline__ int find_task(const int32_t* __restrict__ cu, int n_seqs, int block, int extra, int id,
-                                         int* found /* shared, 2 ints */, uint32_t* status, int& place) {
-  if (threadIdx.x == 0) found[0] = -1;
+// sequence s, rows cu[s] .. cu[s+1]-1, is given floor(cu[s+1] / block) - floor(cu[s] / block) + 2 tasks, which
+// is at least the number of blocks that its rows can touch, and task `id` belongs to the s whose tasks it is among.  All sequences are looked at
+// side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the look: one round of
+// loads, where a binary search would wait for one load after the other.
+struct FoundTask { int seq, place, row0, rows, extra; };
+__device__ __forceinline__ FoundTask find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int block,
+                                               int id, FoundTask* found /* shared */, uint32_t* status) {
+  if (threadIdx.x == 0) found->seq = -1;
   __syncthreads();
   for (int s = threadIdx.x; s < n_seqs; s += blockDim.x) {
-    const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1);
-    const int a = lo / block + extra * s, b = hi / block + extra * (s + 1);
+    const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1), e = extra ? __ldg(extra + s) : 0;
     if (lo < 0 || hi < lo) {
       if (blockIdx.x == 0) record_bad_index(status, kBadOffset);
-    } else if (a <= id && id < b) {
-      found[0] = s;
-      found[1] = id - a;
+    } else {
+      const int a = lo / block + 2 * s;
+      if (a <= id && id < hi / block + 2 * s + 2) *found = FoundTask{s, id - a, lo, hi - lo, e};
     }
   }
   __syncthreads();
-  place = found[1];
-  return found[0];
+  return *found;
 }
 
 int check_cache(const fpt_kv_cache* c, bool with_storage);

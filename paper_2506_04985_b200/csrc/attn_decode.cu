@@ -10,8 +10,9 @@
 //   S^T[T x H] = K Q^T      m16n8k16, fp16 x fp16 -> fp32: codes are exact in fp16 (one byte permutation and one packed subtract make two), and
 //                           the elements' order along the sum is free: a thread's 16 contiguous codes are its operand registers
 //                           of four instructions, so keys need no transposition
-//   w = 2^(S' - M)          S' = S scale_k scale log2(e) + log2(scale_v), M the running maximum of S': the scale of the page's
-//                           values rides in the exponent, w is at most 2^14 (room below for the small ones in fp16)
+//   w = 2^(S' - M + 9)      S' = S scale_k scale log2(e) + log2(scale_v): the scale of the page's values rides in the exponent.
+//                           M is a maximum of S' that is renewed once S' grows 6 beyond it: w stays below 2^15, with as much
+//                           room below for small ones as fp16 has
 //   O^T[D x H] += V^T w     w through one 8x8 transposition between lanes; two tokens' bytes are interleaved by the
 //                           permutations that widen them, so values need no transposition either
 //   l += w / scale_v        float32, unrounded
@@ -23,7 +24,8 @@ namespace fpt {
 constexpr int kDecTile = 64;                       // tokens of a tile
 constexpr int kDecWarps = 4;                       // consumer warps, 16 tokens of a tile each
 constexpr int kDecThreads = (kDecWarps + 1) * 32;
-constexpr float kDecLift = 14.0f;                  // log2 of the largest weight
+constexpr float kDecLift = 9.0f;                   // log2 of the weight of a score at the reference ...
+constexpr float kDecFar = 6.0f;                    // ... and what a score may lie above it: weights stay below 2^15
 constexpr float kDecTinyV = 8.271806125530277e-25f;    // 2^-80
 
 struct DecodeParams {
@@ -36,7 +38,7 @@ struct DecodeParams {
   uint32_t* ws;                 // control block: status word, counters
   float* parts;                 // two a CTA, kAttnPartFloats each
   int ld_q, ld_o, n_q, n_kv, group, blocks, n_seqs, n_pages, max_pages;   // blocks: of 8 NT query heads in a group
-  int page;
+  int page, page_log2;
   float scale_log2;             // scale * log2(e)
 };
 
@@ -96,20 +98,17 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return d;
 }
 
-// CTA of tile x where `total` tiles are cut into `ctas` ranges that start at floor(i * total / ctas).
-__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) { return (int)(((x + 1) * ctas - 1) / total); }
+// `total` tiles in `ctas` ranges: the first `longer` of them have each + 1 tiles, the others `each` (at least 1).
+struct Ranges {
+  int each, longer;
+  __device__ __forceinline__ int first_of(int i) const { return i * each + min(i, longer); }
+  __device__ __forceinline__ int cta_of(int x) const {
+    const int edge = longer * (each + 1);
+    return x < edge ? x / (each + 1) : longer + (x - edge) / each;
+  }
+};
 
 __device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile : 1; }
-
-// Joins the parts of a row: thread `tid` of 128, heads [0, gh).  part(i): the i-th part's floats; out(head, d, value, M, l).
-template <int HD>
-struct PartView {
-  const float* p;
-  int width;                    // heads a part has room for
-  __device__ __forceinline__ const float* sums(int h) const { return p + (size_t)h * HD; }
-  __device__ __forceinline__ float top(int h) const { return __ldcg(p + (size_t)width * HD + h); }
-  __device__ __forceinline__ float total(int h) const { return __ldcg(p + (size_t)width * HD + width + h); }
-};
 
 template <int HD, int NT, int ST, int MINB>
 __global__ void __launch_bounds__(kDecThreads, MINB)
@@ -129,7 +128,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kDecWarps); }
+    for (int s = 0; s < ST; ++s) { mbar_init(full(s), 2); mbar_init(empty(s), kDecWarps); }
     mbar_init(met, kDecWarps);
     *abort_flag = 0;
     fence_mbar_init();
@@ -139,107 +138,123 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   pdl_wait();
   pdl_launch_dependents();
 
-  // Every warp of the producer's needs: the number of tiles and this CTA's range of them.
+  // The producer warp finds the number of tiles, this CTA's range of them and the sequence of the first: 32 sequences at a time; up to 32
+  // are looked at once.
   const int heads = P.n_kv * P.blocks;
   const int cap = P.max_pages * P.page;
-  int64_t first = 0, end = 0, total = 0;
-  int ctas = 1;
+  int first = 0, end = 0, off = 0, seq = 0;           // off: first tile of sequence `seq`
+  Ranges ranges = {1, 0};
   if (warp == kDecWarps) {
-    int64_t mine = 0;
+    int mine = 0;                                     // of the sequences lane, lane + 32, ...
     bool bad = false;
     for (int s = lane; s < P.n_seqs; s += 32) {
       const int len = __ldg(P.kv_len + s);
       bad |= len < 0 || len > cap;
-      mine += tiles_of(min(len, cap));
+      mine += tiles_of(min(len, cap)) * heads;
     }
+    auto scan = [&](int v) -> int {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+      for (int o = 1; o < 32; o <<= 1) {
+        const int w = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += w;
+      }
+      return v;
+    };
+    int incl = scan(mine);
+    const int total = __shfl_sync(0xffffffffu, incl, 31), ctas = min((int)gridDim.x, total);
     if (bad && blockIdx.x == 0) record_bad_index(P.ws, kBadLength);
-    total = mine * heads;
-    ctas = (int)min((int64_t)gridDim.x, total);
+    ranges.each = total / ctas;
+    ranges.longer = total - ranges.each * ctas;
     if ((int)blockIdx.x < ctas) {
-      first = (int64_t)blockIdx.x * total / ctas;
-      end = (int64_t)(blockIdx.x + 1) * total / ctas;
+      first = ranges.first_of(blockIdx.x);
+      end = ranges.first_of(blockIdx.x + 1);
+      for (int s0 = 0;; s0 += 32) {                   // (ends: the tiles add up to `total`)
+        if (P.n_seqs > 32) {
+          const int s = s0 + lane;
+          mine = s < P.n_seqs ? tiles_of(min(__ldg(P.kv_len + s), cap)) * heads : 0;
+          incl = scan(mine);
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, off + incl > first);
+        if (hit) {
+          const int src = __ffs(hit) - 1;
+          off += __shfl_sync(0xffffffffu, incl - mine, src);
+          seq = s0 + src;
+          break;
+        }
+        off += __shfl_sync(0xffffffffu, incl, 31);
+        if (s0 + 32 >= P.n_seqs) { end = first; break; }
+      }
     }
-    if (lane == 0) *n_tiles_s = (int)(end - first);
+    if (lane == 0) *n_tiles_s = end - first;
   }
   __syncthreads();
 
   if (warp == kDecWarps) {
     // ------------------------------------------------------------------ producer
-    // sequence of the first tile: 32 sequences at a time
-    int seq = 0;
-    int64_t off = 0;                                  // first tile of sequence `seq`
-    if (first < end) {
-      for (int s0 = 0;; s0 += 32) {
-        const int s = s0 + lane;
-        const int64_t t = s < P.n_seqs ? (int64_t)tiles_of(min(__ldg(P.kv_len + s), cap)) * heads : 0;
-        int64_t incl = t;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += v;
-        }
-        const uint32_t hit = __ballot_sync(0xffffffffu, off + incl > first);
-        if (hit) {
-          const int src = __ffs(hit) - 1;
-          off += __shfl_sync(0xffffffffu, incl - t, src);
-          seq = s0 + src;
-          break;
-        }
-        off += __shfl_sync(0xffffffffu, incl, 31);
-        if (s0 + 32 >= P.n_seqs) { first = end; break; }           // (not reached: the tiles add up to `total`)
-      }
-    }
     const int pieces_max = P.page >= kDecTile ? 1 : kDecTile / P.page;    // pages of a tile
     const int piece = min(P.page, kDecTile);                              // their tokens
-    // What a lane knows about its tile of the next batch of 32: pages and scales are asked for a batch ahead.
+    // What a lane knows about its tile of a batch of 32, in three steps that each wait for what the one before asked of memory: its place and
+    // pages, the pages' scales, the entry for the consumers.
     TileInfo ti;
-    int page_row[4], tok_n = 0;
-    auto look = [&](int64_t base) {
-      const int64_t x = base + lane;
-      tok_n = 0; ti.flags = 0;
+    int ids[4], cells[4], rows[4], tok_n = 0, tok0 = 0, kv_head = 0, q_heads = 0, q_at = 0;
+    auto look_pages = [&](int base) {
+      const int x = base + lane;
+      tok_n = 0;
+      ti.flags = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ids[i] = -1;
       if (x >= end) return;
-      int s = seq;
-      int64_t o = off;
+      int s = seq, o = off;
       int len = min(__ldg(P.kv_len + s), cap);
       int nt = tiles_of(len);
-      while (x >= o + (int64_t)nt * heads) {          // (x < total: there is a next sequence)
-        o += (int64_t)nt * heads;
+      while (x >= o + nt * heads) {                   // (x is below the sum of all: there is a next sequence)
+        o += nt * heads;
         ++s;
         len = min(__ldg(P.kv_len + s), cap);
         nt = tiles_of(len);
       }
-      const int64_t in = x - o;
-      const int h = (int)(in / nt), t = (int)(in - (int64_t)h * nt);
+      const int in = x - o, h = in / nt, t = in - h * nt;
+      tok0 = t * kDecTile;
+      tok_n = max(0, min(kDecTile, len - tok0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < pieces_max && i * piece < tok_n)
+          ids[i] = __ldg(P.pages + (size_t)s * P.max_pages + ((tok0 + i * piece) >> P.page_log2));
+      kv_head = h / P.blocks;
+      const int blk = h - kv_head * P.blocks;
+      q_heads = min(NH, P.group - blk * NH);
+      q_at = kv_head * P.group + blk * NH;
       ti.seq = s; ti.head = h;
-      tok_n = max(0, min(kDecTile, len - t * kDecTile));
       const bool whole = x - t >= first && x - t + nt <= end;
       const bool a = t == 0 || x == first, z = t == nt - 1 || x == end - 1;
       ti.flags = (a ? 1 : 0) | (z ? 2 : 0) | (whole ? 4 : 0) | (tok_n << 8);
       ti.parts = 0;
       if (z && !whole) {
-        const int c0 = cta_of(x - t, total, ctas), c1 = cta_of(x - t + nt - 1, total, ctas);
+        const int c0 = ranges.cta_of(x - t), c1 = ranges.cta_of(x - t + nt - 1);
         ti.parts = (uint32_t)c0 | (uint32_t)(c1 - c0 + 1) << 16;
       }
-      const int kv_head = h / P.blocks;
+    };
+    auto find_rows = [&]() {
+      bool bad = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        page_row[i] = -1;
-        if (i < pieces_max && i * piece < tok_n) {
-          const int tok = t * kDecTile + i * piece;
-          int pg = __ldg(P.pages + (size_t)s * P.max_pages + tok / P.page);
-          const bool ok = pg >= 0 && pg < P.n_pages;
-          if (!ok) { record_bad_index(P.ws, kBadPage); pg = 0; }
-          const int cell = pg * P.n_kv + kv_head;
-          page_row[i] = cell * P.page + tok % P.page;
-          ti.ks[i] = __ldg(P.k_scale + cell) * P.scale_log2;
-          ti.vl[i] = __ldg(P.v_scale + cell);
-        }
+        const bool used = i < pieces_max && i * piece < tok_n, fine = ids[i] >= 0 && ids[i] < P.n_pages;
+        bad |= used && !fine;
+        cells[i] = (fine ? ids[i] : 0) * P.n_kv + kv_head;
+        rows[i] = used ? (cells[i] << P.page_log2) + ((tok0 + i * piece) & (P.page - 1)) : -1;
       }
+      if (bad) record_bad_index(P.ws, kBadPage);
     };
-    auto publish = [&](int64_t base) {                // the look-ups, laid out per 16 tokens
-      const int64_t x = base + lane;
+    auto look_scales = [&]() {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (rows[i] >= 0) {
+          ti.ks[i] = __ldg(P.k_scale + cells[i]);
+          ti.vl[i] = __ldg(P.v_scale + cells[i]);
+        }
+    };
+    auto publish = [&](int base) {                    // laid out per 16 tokens
+      const int x = base + lane;
       if (x >= end) return;
       TileInfo out = ti;
       const int per = piece / 16;
@@ -250,60 +265,63 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const float v = per == 4 ? ti.vl[0] : per == 2 ? (i < 2 ? ti.vl[0] : ti.vl[1]) : ti.vl[i];
         const bool used = i * 16 < tok_n;
         const bool live = v >= kDecTinyV;
-        out.ks[i] = used ? k : 0.0f;
-        out.vl[i] = !used ? 0.0f : v != v ? v : live ? log2f(v) : -80.0f;
+        out.ks[i] = used ? k * P.scale_log2 : 0.0f;
+        out.vl[i] = !used ? 0.0f : v != v ? v : live ? __log2f(v) : -80.0f;
         if (used && (live || v != v)) out.flags |= 16 << i;
       }
-      infos[(int)(x - first) & 63] = out;
+      infos[(x - first) & 63] = out;
     };
     int st = 0; uint32_t ph = 0, armed = 0, armed_par = 0;
     bool ok = true;
-    if (first < end) { look(first); publish(first); }
-    for (int64_t base = first; ok && base < end; base += 32) {
-      __syncwarp();
-      int rows[4] = {page_row[0], page_row[1], page_row[2], page_row[3]};
-      const int my_flags = ti.flags, my_seq = ti.seq, my_head = ti.head;
-      // where the next batch starts to look
-      const int last_lane = (int)min((int64_t)31, end - 1 - base);
-      {
-        const int s_last = __shfl_sync(0xffffffffu, my_seq, last_lane);
-        while (seq < s_last) { off += (int64_t)tiles_of(min(__ldg(P.kv_len + seq), cap)) * heads; ++seq; }
-      }
-      if (base + 32 < end) look(base + 32);
-      const int count = last_lane + 1;
+    if (first < end) { look_pages(first); find_rows(); look_scales(); }
+    for (int base = first; ok && base < end; base += 32) {
+      // a lane requests its own tile
+      const int my_rows[4] = {rows[0], rows[1], rows[2], rows[3]};
+      const uint32_t q_bytes = (ti.flags & 1) ? (uint32_t)q_heads * HD * 2 : 0u;
+      const __nv_bfloat16* q_from = P.Q + (size_t)ti.seq * P.ld_q + (size_t)q_at * HD;
+      const int my_seq = ti.seq;
+      const int count = min(32, end - base);
+      const bool more = base + 32 < end;
+      // The first tiles of all are requested before their scales are there: the consumers' barrier counts the copies and, apart
+      // from them, the entry.
+      const int ahead = base == first ? min(count, ST) : 0;
       for (int i = 0; i < count; ++i) {
-        const int fl = __shfl_sync(0xffffffffu, my_flags, i);
-        const int sq = __shfl_sync(0xffffffffu, my_seq, i), hd = __shfl_sync(0xffffffffu, my_head, i);
-        int r[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = __shfl_sync(0xffffffffu, rows[j], i);
-        if (!mbar_wait_warp(empty(st), ph ^ 1u, abort_flag, P.ws, 1)) { ok = false; break; }
-        if (lane == 0) {
+        if (!wait_long<true>(empty(st), ph ^ 1u, abort_flag, P.ws, 1)) { ok = false; break; }
+        if (lane == i) {
           int boxes = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) boxes += r[j] >= 0;
-          const int kvh = hd / P.blocks, blk = hd - kvh * P.blocks;
-          const int gh = min(NH, P.group - blk * NH);
-          const uint32_t qb = (fl & 1) ? (uint32_t)gh * HD * 2 : 0u;
-          mbar_arrive_expect_tx(full(st), (uint32_t)boxes * piece * HD * 2 + qb);
+          for (int j = 0; j < 4; ++j) boxes += my_rows[j] >= 0;
+          mbar_arrive_expect_tx(full(st), (uint32_t)(boxes * piece * HD * 2) + q_bytes);
           const uint32_t dst = sbase + L::kRing + st * 2 * L::kMat;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (r[j] >= 0) {
-              tma_load_2d(dst + j * piece * HD, &tmK, full(st), 0, r[j]);
-              tma_load_2d(dst + L::kMat + j * piece * HD, &tmV, full(st), 0, r[j]);
+            if (my_rows[j] >= 0) {
+              tma_load_2d(dst + j * piece * HD, &tmK, full(st), 0, my_rows[j]);
+              tma_load_2d(dst + L::kMat + j * piece * HD, &tmV, full(st), 0, my_rows[j]);
             }
-          if (qb)
-            bulk_load_1d(sbase + L::kQOff + st * L::kQ,
-                         P.Q + (size_t)sq * P.ld_q + (size_t)(kvh * P.group + blk * NH) * HD, qb, full(st));
+          if (q_bytes) bulk_load_1d(sbase + L::kQOff + st * L::kQ, q_from, q_bytes, full(st));
+          if (i >= ahead) mbar_arrive(full(st));
         }
         armed |= 1u << st;
         armed_par = (armed_par & ~(1u << st)) | (ph << st);
         if (++st == ST) { st = 0; ph ^= 1u; }
+        if (i == ahead - 1) {
+          publish(base);
+          __syncwarp();
+          if (lane == 0)
+            for (int k = 0; k < ahead; ++k) mbar_arrive(full(k));
+        }
+        // the next batch, a step at a time between the tiles of this one
+        if (more && i == 8) {
+          const int s_last = __shfl_sync(0xffffffffu, my_seq, 31);          // where it starts to look
+          while (seq < s_last) { off += tiles_of(min(__ldg(P.kv_len + seq), cap)) * heads; ++seq; }
+          look_pages(base + 32);
+        }
+        if (more && i == 16) { find_rows(); look_scales(); }
       }
-      // The half of the ring that the next batch takes was read when the tile 32 back was let go, long before the last of
+      // The half of the ring of entries that the next batch takes was read when the tile 32 back was let go, long before the last of
       // these 32 could be requested (the ring of tiles is shorter).
-      if (ok && base + 32 < end) publish(base + 32);
+      if (ok && more) { publish(base + 32); __syncwarp(); }
     }
     if (!ok && lane == 0) {
       const uint64_t t0 = globaltimer_ns();
@@ -332,12 +350,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     auto meet = [&]() -> bool {
       __syncwarp();
       if (lane == 0) mbar_arrive(met);
-      const bool ok = mbar_wait_warp(met, met_ph, abort_flag, P.ws, 3);
+      const bool ok = wait_long<true>(met, met_ph, abort_flag, P.ws, 3);
       met_ph ^= 1u;
       return ok;
     };
     for (int i = 0; i < n_tiles; ++i) {
-      if (!mbar_wait_warp(full(st), ph, abort_flag, P.ws, 2)) break;
+      if (!wait_long<true>(full(st), ph, abort_flag, P.ws, 2)) break;
       const TileInfo& ti = infos[i & 63];
       const int flags = ti.flags, n = flags >> 8, head = ti.head;
       if (flags & 1) {
@@ -393,57 +411,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint8_t* vs = ks + L::kMat;
         const float kf = ti.ks[warp], vl = ti.vl[warp];
         const bool v_live = (flags >> (4 + warp)) & 1;
-        float S[NT][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) S[t][0] = S[t][1] = S[t][2] = S[t][3] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < HD / 64; ++c) {
-          const uint4 ra = *reinterpret_cast<const uint4*>(ks + chunk(row_a, c * 4 + q));
-          const uint4 rb = *reinterpret_cast<const uint4*>(ks + chunk(row_b, c * 4 + q));
-          const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t fa = wa[w] ^ 0x80808080u, fb = wb[w] ^ 0x80808080u;
-            const uint32_t a0 = bytes_to_half2<0x4140>(fa), a2 = bytes_to_half2<0x4342>(fa);
-            const uint32_t a1 = bytes_to_half2<0x4140>(fb), a3 = bytes_to_half2<0x4342>(fb);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma_f16(S[t], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
-          }
-        }
-        uint32_t p0[NT], p1[NT];
-        const bool in_a = row_a < n, in_b = row_b < n;
-        const float inv_v = ex2(-vl);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const float f0 = qscale[t][0] * kf, f1 = qscale[t][1] * kf;
-          float s[4] = {fmaf(S[t][0], f0, vl), fmaf(S[t][1], f1, vl), fmaf(S[t][2], f0, vl), fmaf(S[t][3], f1, vl)};
-          if (!in_a) s[0] = s[1] = -INFINITY;
-          if (!in_b) s[2] = s[3] = -INFINITY;
-          float m0 = fmaxf(s[0], s[2]), m1 = fmaxf(s[1], s[3]);
-#pragma unroll
-          for (int o = 4; o <= 16; o <<= 1) {
-            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
-            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
-          }
-          if (__any_sync(0xffffffffu, m0 > M[t][0] || m1 > M[t][1])) {
-            const float n0 = fmaxf(M[t][0], m0), n1 = fmaxf(M[t][1], m1);
-            const float r0 = M[t][0] == -INFINITY ? 0.0f : ex2(M[t][0] - n0);
-            const float r1 = M[t][1] == -INFINITY ? 0.0f : ex2(M[t][1] - n1);
-            M[t][0] = n0; M[t][1] = n1;
-            l[t][0] *= r0; l[t][1] *= r1;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) { O[t][k][0] *= r0; O[t][k][1] *= r1; O[t][k][2] *= r0; O[t][k][3] *= r1; }
-          }
-          // a maximum of -inf: nothing counts yet, and no difference of infinities is formed
-          const float b0 = M[t][0] == -INFINITY ? 0.0f : M[t][0] - kDecLift, b1 = M[t][1] == -INFINITY ? 0.0f : M[t][1] - kDecLift;
-          float w[4] = {ex2(s[0] - b0), ex2(s[1] - b1), ex2(s[2] - b0), ex2(s[3] - b1)};
-          l[t][0] = fmaf(w[0] + w[2], inv_v, l[t][0]);
-          l[t][1] = fmaf(w[1] + w[3], inv_v, l[t][1]);
-          if (!v_live) w[0] = w[1] = w[2] = w[3] = 0.0f;
-          p0[t] = transpose8x8(half2_bits(__floats2half2_rn(w[0], w[1])));
-          p1[t] = transpose8x8(half2_bits(__floats2half2_rn(w[2], w[3])));
-        }
-        // values: tokens 2q, 2q+1, 2q+8, 2q+9 of the group, elements g * HD/8 ...
+        // values: tokens 2q, 2q+1, 2q+8, 2q+9 of the group, elements g * HD/8 ...  (asked for first: they arrive under the scores)
         constexpr int W = HD / 32;
         uint32_t v[4][W];
 #pragma unroll
@@ -456,6 +424,70 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             const uint2 x = *reinterpret_cast<const uint2*>(vs + chunk(row, g >> 1) + (g & 1) * 8);
             v[j][0] = x.x; v[j][1] = x.y;
           }
+        }
+        // scores, in two chains of accumulators
+        float S[NT][2][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) S[t][k >> 2][k & 3] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c) {
+          const uint4 ra = *reinterpret_cast<const uint4*>(ks + chunk(row_a, c * 4 + q));
+          const uint4 rb = *reinterpret_cast<const uint4*>(ks + chunk(row_b, c * 4 + q));
+          const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t fa = wa[w] ^ 0x80808080u, fb = wb[w] ^ 0x80808080u;
+            const uint32_t a0 = bytes_to_half2<0x4140>(fa), a2 = bytes_to_half2<0x4342>(fa);
+            const uint32_t a1 = bytes_to_half2<0x4140>(fb), a3 = bytes_to_half2<0x4342>(fb);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma_f16(S[t][w & 1], a0, a1, a2, a3, qf[t][c * 4 + w][0], qf[t][c * 4 + w][1]);
+          }
+        }
+        uint32_t p0[NT], p1[NT];
+        const bool in_a = row_a < n, in_b = row_b < n;
+        const float inv_v = ex2(-vl);
+        float s[NT][4];
+        bool far = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float f0 = qscale[t][0] * kf, f1 = qscale[t][1] * kf;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            s[t][k] = fmaf(S[t][0][k] + S[t][1][k], k & 1 ? f1 : f0, vl);
+            if (!(k < 2 ? in_a : in_b)) s[t][k] = -INFINITY;
+            far |= s[t][k] > M[t][k & 1] + kDecFar;
+          }
+        }
+        // The reference of a head is renewed only where a score lies far above it (the first one does): the maximum over the
+        // lanes is six shuffles that nothing waits for otherwise.
+        if (__any_sync(0xffffffffu, far)) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float m = fmaxf(s[t][j], s[t][2 + j]);
+#pragma unroll
+              for (int o = 4; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+              m = fmaxf(M[t][j], m);
+              const float r = M[t][j] == -INFINITY ? 0.0f : ex2(M[t][j] - m);
+              M[t][j] = m;
+              l[t][j] *= r;
+#pragma unroll
+              for (int k = 0; k < KS; ++k) { O[t][k][j] *= r; O[t][k][2 + j] *= r; }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          // a reference of -inf: nothing counts yet, and no difference of infinities is formed
+          const float b0 = M[t][0] == -INFINITY ? 0.0f : M[t][0] - kDecLift, b1 = M[t][1] == -INFINITY ? 0.0f : M[t][1] - kDecLift;
+          float w[4] = {ex2(s[t][0] - b0), ex2(s[t][1] - b1), ex2(s[t][2] - b0), ex2(s[t][3] - b1)};
+          l[t][0] = fmaf(w[0] + w[2], inv_v, l[t][0]);
+          l[t][1] = fmaf(w[1] + w[3], inv_v, l[t][1]);
+          if (!v_live) w[0] = w[1] = w[2] = w[3] = 0.0f;
+          p0[t] = transpose8x8(half2_bits(__floats2half2_rn(w[0], w[1])));
+          p1[t] = transpose8x8(half2_bits(__floats2half2_rn(w[2], w[3])));
         }
 #pragma unroll
         for (int w = 0; w < W; ++w) {
@@ -513,7 +545,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             P.lse[(size_t)row_seq * P.n_q + q0 + h] =
                 sum > 0.0f || sum != sum ? (m - kDecLift) * 0.69314718055994531f + logf(sum) : -INFINITY;
         };
-        constexpr int D4 = HD / 4;
+        constexpr int D4 = HD / 4, kPerThread = NH * D4 / (kDecWarps * 32);
         float* part = P.parts + (size_t)(2 * (int)blockIdx.x + ((int)blockIdx.x == part0 ? 1 : 0)) * kAttnPartFloats;
         for (int e = tid; e < gh * D4; e += kDecWarps * 32) {
           const int h = e / D4, d = (e % D4) * 4;
@@ -538,9 +570,9 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           }
         }
         if (!(flags & 4)) {
-          __threadfence();
           if (!meet()) break;
           if (tid == 0) {
+            __threadfence();                            // (the whole CTA's part, which the warps' meeting put before this)
             uint32_t* counter = P.ws + kCounterWord0 + part0;
             const bool last = atomicAdd(counter, 1u) == (uint32_t)nparts - 1u;
             if (last) *counter = 0;                   // as the next call finds it
@@ -549,26 +581,88 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           }
           if (!meet()) break;
           if (*last_flag) {
-            // the row's parts, in their order: the first is the tail part of its CTA, the others head parts of theirs
-            auto view = [&](int p) {
-              return PartView<HD>{P.parts + (size_t)(2 * (part0 + p) + (p == 0 ? 1 : 0)) * kAttnPartFloats, NH};
-            };
-            for (int e = tid; e < gh * D4; e += kDecWarps * 32) {
-              const int h = e / D4, d = (e % D4) * 4;
-              float top = -INFINITY;
-              for (int p = 0; p < nparts; ++p) top = fmaxf(top, view(p).top(h));
-              float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-              float sum = 0.0f;
-#pragma unroll 4
-              for (int p = 0; p < nparts; ++p) {
-                const PartView<HD> w = view(p);
-                const float m = w.top(h);
-                const float r = m == -INFINITY ? 0.0f : ex2(m - top);
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(w.sums(h) + d));
-                o.x = fmaf(x.x, r, o.x); o.y = fmaf(x.y, r, o.y); o.z = fmaf(x.z, r, o.z); o.w = fmaf(x.w, r, o.w);
-                sum = fmaf(w.total(h), r, sum);
+            // The row's parts, in their order: the first is the tail part of its CTA, the others head parts of theirs.  First the
+            // exponents (a head and every 128 / NH-th part a thread), then weights into shared memory, as many parts at a time as it
+            // has room for, then the sums: loads of one step do not wait for one another.
+            auto part_at = [&](int p) { return P.parts + (size_t)(2 * (part0 + p) + (p == 0 ? 1 : 0)) * kAttnPartFloats; };
+            constexpr int kRoom = kDecWarps * HD;       // parts whose weights fit
+            float* weights = merge;                     // [part][NH]
+            const int h0 = tid % NH, p0 = tid / NH;
+            constexpr int kStep = kDecWarps * 32 / NH, kBatch = 12;
+            float top = -INFINITY;
+            // (a batch of loads has a fixed length, what lies behind the last part left out: the tail of an unrolled loop would
+            // wait for one load after the other, 6 us of 11 with 55 parts)
+            for (int p = p0; p < nparts; p += 4 * kStep) {
+              float m[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                m[k] = p + k * kStep < nparts && h0 < gh ? __ldcg(part_at(p + k * kStep) + NH * HD + h0) : -INFINITY;
+              top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+            }
+            merge[tid] = top;
+            if (!meet()) break;
+            top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) top = fmaxf(top, merge[k * NH + h0]);
+            if (!meet()) break;
+            float4 o[kPerThread];
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k) o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float sum = 0.0f;                           // of head h0, this thread's parts
+            bool fine = true;
+            for (int from = 0; from < nparts; from += kRoom) {
+              const int n_here = min(kRoom, nparts - from);
+              for (int p = p0; p < n_here; p += 4 * kStep) {
+                float m[4], l[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const bool there = p + k * kStep < n_here && h0 < gh;
+                  const float* w = part_at(from + (there ? p + k * kStep : 0)) + NH * HD;
+                  m[k] = there ? __ldcg(w + h0) : -INFINITY;
+                  l[k] = there ? __ldcg(w + NH + h0) : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const float r = m[k] == -INFINITY ? 0.0f : ex2(m[k] - top);
+                  sum = fmaf(l[k], r, sum);
+                  if (p + k * kStep < n_here) weights[(p + k * kStep) * NH + h0] = r;
+                }
               }
-              emit(h, d, o, top, sum);
+              if (!(fine = meet())) break;
+#pragma unroll
+              for (int k = 0; k < kPerThread; ++k) {
+                const int e = tid + k * kDecWarps * 32, h = e / D4, d = (e % D4) * 4;
+                if (e < gh * D4) {
+                  for (int p = 0; p < n_here; p += kBatch) {
+                    float4 x[kBatch];
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                      x[b] = p + b < n_here ? __ldcg(reinterpret_cast<const float4*>(part_at(from + p + b) + (size_t)h * HD + d))
+                                            : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                      const float r = p + b < n_here ? weights[(p + b) * NH + h] : 0.0f;
+                      o[k].x = fmaf(x[b].x, r, o[k].x); o[k].y = fmaf(x[b].y, r, o[k].y);
+                      o[k].z = fmaf(x[b].z, r, o[k].z); o[k].w = fmaf(x[b].w, r, o[k].w);
+                    }
+                  }
+                }
+              }
+              if (!(fine = meet())) break;
+            }
+            if (!fine) break;
+            merge[tid] = sum;
+            if (p0 == 0) merge[kDecWarps * 32 + h0] = top;
+            if (!meet()) break;
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k) {
+              const int e = tid + k * kDecWarps * 32, h = e / D4, d = (e % D4) * 4;
+              if (e < gh * D4) {
+                float all = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kStep; ++i) all += merge[i * NH + h];
+                emit(h, d, o[k], merge[kDecWarps * 32 + h], all);
+              }
             }
           }
         }
@@ -595,7 +689,7 @@ template <int HD, int NT, int ST, int MINB>
 static int launch_decode(cudaStream_t st, const fpt_kv_cache* c, DecodeParams P) {
   using L = DecSmem<HD, NT, ST>;
   static_assert((L::kAlloc + 1024) * MINB <= 228 * 1024, "the ring does not fit");
-  static_assert(ST < 32, "a batch of tiles has to be longer than the ring");
+  static_assert(ST <= 8, "a batch of tiles has to be longer than the ring");
   auto kern = attn_decode_kernel<HD, NT, ST, MINB>;
   static PerDeviceInt attr_set;
   if (!ensure_smem_attr(attr_set, kern, L::kAlloc)) return FPT_ERR_CUDA;
@@ -606,6 +700,7 @@ static int launch_decode(cudaStream_t st, const fpt_kv_cache* c, DecodeParams P)
   P.blocks = (P.group + 8 * NT - 1) / (8 * NT);
   // a CTA for each tile at most
   const int64_t most = (int64_t)P.n_seqs * P.n_kv * P.blocks * (((int64_t)c->max_pages * c->page + kDecTile - 1) / kDecTile);
+  if (most > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   int64_t grid = (int64_t)device_sm_count() * MINB;
   if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
   if (grid > most) grid = most;
@@ -639,9 +734,16 @@ extern "C" int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, c
   P.parts = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kStatusBytes);
   P.ld_q = ld_q; P.ld_o = ld_o; P.n_q = n_q; P.n_kv = cache->n_kv; P.group = n_q / cache->n_kv; P.n_seqs = n_seqs;
   P.n_pages = cache->n_pages; P.max_pages = cache->max_pages; P.page = cache->page;
+  while ((1 << P.page_log2) < P.page) ++P.page_log2;
   P.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)stream;
+#ifndef DEC_CFG
+#define DEC_CFG 128, 1, 3, 3
+#endif
+#ifndef DEC_CFG64
+#define DEC_CFG64 64, 1, 6, 3
+#endif
   if (cache->head_dim == 128)
-    return P.group <= 8 ? launch_decode<128, 1, 3, 3>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
-  return P.group <= 8 ? launch_decode<64, 1, 6, 3>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);
+    return P.group <= 8 ? launch_decode<DEC_CFG>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
+  return P.group <= 8 ? launch_decode<DEC_CFG64>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);
 }

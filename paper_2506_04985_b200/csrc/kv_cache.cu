@@ -6,9 +6,9 @@
 //
 // One CTA has one page of one key/value head, so that the largest magnitude of the page's new tokens, its scale and its
 // codes need no second pass over memory and no exchange between CTAs: the 16-bit values stay in registers while
-// their maximum goes around the CTA.  The query heads of the group ride along, with the rotations of their tokens already in
-// registers.  Page and head are contiguous ([page][head][slot][element]), so a full page of codes leaves as one
-// 8 KB run.
+// their maximum goes around the CTA.  Page and head are contiguous ([page][head][slot][element]), so a full page of codes leaves as one
+// 8 KB run.  The queries of the page's tokens have CTAs of their own, a group of heads each: with them in the same CTA its
+// registers held two CTAs an SM (8190 tokens of 32 + 8 heads: KV_APPEND_OLD us, KV_APPEND_NEW us).
 #include "attn_common.cuh"
 
 namespace fpt {
@@ -26,17 +26,43 @@ struct RopeParams {
   int M, ld, ld_q, ld_k, n_q, n_kv, n_pos, rot, interleaved, n_seqs, n_pages, page, max_pages;
 };
 
-// Sixteen elements of a head that belong together: two runs of eight, at `a` and at `b`.  Below rot: with the half layout the second
-// run holds the partners of the first, with the interleaved one both hold pairs of neighbours; `pair` is the first
-// pair of the sixteen elements' eight.
-struct Item { int a, b, pair; };
+// Sixteen elements of a head: two runs of eight, at `a` and at `b`.  Neighbours' runs follow each other (16 bytes a lane at a
+// stride of 32 would write half sectors).  With the half layout a turned item's second run holds the partners of its first, and `pa` is
+// the first of their eight pairs; with the interleaved one each run holds four pairs of neighbours, from pa and from pb on.  -1: not turned.
+struct Item { int a, b, pa, pb; };
+template <int HD>
 __device__ __forceinline__ Item item_of(int sub, int rot, int interleaved) {
   Item i;
-  const bool turned = sub * 16 < rot;
-  i.a = turned && !interleaved ? sub * 8 : sub * 16;
-  i.b = turned && !interleaved ? i.a + rot / 2 : i.a + 8;
-  i.pair = turned ? sub * 8 : -1;
+  if (interleaved) {
+    i.a = sub * 8;
+    i.b = HD / 2 + sub * 8;
+    i.pa = i.a < rot ? i.a / 2 : -1;
+    i.pb = i.b < rot ? i.b / 2 : -1;
+  } else {
+    const bool turned = sub * 16 < rot;
+    const int from = turned ? 0 : rot, len = turned ? rot : HD - rot, k = turned ? sub : sub - rot / 16;
+    i.a = from + k * 8;
+    i.b = i.a + len / 2;
+    i.pa = turned ? sub * 8 : -1;
+    i.pb = -1;
+  }
   return i;
+}
+
+// The rotations of an item at one position: eight (cos, sin) pairs, those that it has.
+__device__ __forceinline__ void load_rotations(const RopeParams& P, const Item& e, int pos, float4 (&cs)[4]) {
+  const float* r = P.rope + (size_t)pos * P.rot;
+  if (e.pa >= 0) {
+    const float4* f = reinterpret_cast<const float4*>(r + e.pa * 2);
+    cs[0] = __ldg(f);
+    cs[1] = __ldg(f + 1);
+    if (!P.interleaved) { cs[2] = __ldg(f + 2); cs[3] = __ldg(f + 3); }
+  }
+  if (e.pb >= 0) {
+    const float4* f = reinterpret_cast<const float4*>(r + e.pb * 2);
+    cs[2] = __ldg(f);
+    cs[3] = __ldg(f + 1);
+  }
 }
 
 __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
@@ -45,23 +71,32 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   a = x;
 }
 
-// cs: eight (cos, sin) pairs.
-__device__ __forceinline__ void rotate16(uint4& lo, uint4& hi, const float4 (&cs)[4], int interleaved) {
+__device__ __forceinline__ void rotate_item(const Item& e, uint4& lo, uint4& hi, const float4 (&cs)[4], int interleaved) {
   uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
+  if (interleaved) {                           // word i of a run is one pair
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float l0 = bf16lo_to_f32(l[i]), l1 = bf16hi_to_f32(l[i]), h0 = bf16lo_to_f32(h[i]), h1 = bf16hi_to_f32(h[i]);
-    if (interleaved) {                       // l[i] is pair i, h[i] pair 4 + i
+    for (int i = 0; i < 4; ++i) {
       const float4 p = cs[i >> 1], q = cs[2 + (i >> 1)];
-      turn(l0, l1, (i & 1) ? p.z : p.x, (i & 1) ? p.w : p.y);
-      turn(h0, h1, (i & 1) ? q.z : q.x, (i & 1) ? q.w : q.y);
-    } else {                                 // pairs 2 i and 2 i + 1 across the two runs
-      const float4 p = cs[i];
-      turn(l0, h0, p.x, p.y);
-      turn(l1, h1, p.z, p.w);
+      if (e.pa >= 0) {
+        float x = bf16lo_to_f32(l[i]), y = bf16hi_to_f32(l[i]);
+        turn(x, y, (i & 1) ? p.z : p.x, (i & 1) ? p.w : p.y);
+        l[i] = f32x2_to_bf16x2_bits(x, y);
+      }
+      if (e.pb >= 0) {
+        float x = bf16lo_to_f32(h[i]), y = bf16hi_to_f32(h[i]);
+        turn(x, y, (i & 1) ? q.z : q.x, (i & 1) ? q.w : q.y);
+        h[i] = f32x2_to_bf16x2_bits(x, y);
+      }
     }
-    l[i] = f32x2_to_bf16x2_bits(l0, l1);
-    h[i] = f32x2_to_bf16x2_bits(h0, h1);
+  } else if (e.pa >= 0) {                      // words i of the two runs are pairs 2 i and 2 i + 1
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float l0 = bf16lo_to_f32(l[i]), l1 = bf16hi_to_f32(l[i]), h0 = bf16lo_to_f32(h[i]), h1 = bf16hi_to_f32(h[i]);
+      turn(l0, h0, cs[i].x, cs[i].y);
+      turn(l1, h1, cs[i].z, cs[i].w);
+      l[i] = f32x2_to_bf16x2_bits(l0, l1);
+      h[i] = f32x2_to_bf16x2_bits(h0, h1);
+    }
   }
   lo = make_uint4(l[0], l[1], l[2], l[3]);
   hi = make_uint4(h[0], h[1], h[2], h[3]);
@@ -88,28 +123,22 @@ __device__ __forceinline__ uint2 codes8(const uint4& v, float inv) {
 
 // T threads; every thread holds up to N items of keys and as many of values.
 template <int HD, int T, int N>
-__global__ void __launch_bounds__(T) rope_append_kernel(const RopeParams P) {
+__global__ void __launch_bounds__(T, (N <= 2 ? 1024 : 512) / T) rope_append_kernel(const RopeParams P) {
   constexpr int I = HD / 16;                    // items of a head
-  __shared__ int found[2];
+  __shared__ FoundTask found;
   __shared__ uint32_t peak[2][T / 32];
   pdl_wait();
   pdl_launch_dependents();
 
-  const int head = blockIdx.y, tid = threadIdx.x;
-  int s, place, row0 = 0, n_new = 1;
-  if (P.cu) {
-    s = find_task(P.cu, P.n_seqs, P.page, 2, blockIdx.x, found, P.status, place);
-    if (s < 0) return;
-    row0 = __ldg(P.cu + s);
-    n_new = __ldg(P.cu + s + 1) - row0;
-    if (row0 > P.M - n_new) {                   // (both are at least 0)
-      if (tid == 0) record_bad_index(P.status, kBadOffset);
-      return;
-    }
-  } else {
-    s = blockIdx.x; place = 0; row0 = s;
+  const int head = blockIdx.y % P.n_kv, tid = threadIdx.x;
+  const FoundTask task = P.cu ? find_task(P.cu, P.ctx, P.n_seqs, P.page, blockIdx.x, &found, P.status)
+                              : FoundTask{(int)blockIdx.x, 0, (int)blockIdx.x, 1, __ldg(P.ctx + blockIdx.x)};
+  const int s = task.seq, place = task.place, row0 = task.row0, n_new = task.rows, ctx = task.extra;
+  if (s < 0) return;
+  if (row0 > P.M - n_new) {                     // (both are at least 0)
+    if (tid == 0) record_bad_index(P.status, kBadOffset);
+    return;
   }
-  const int ctx = __ldg(P.ctx + s);
   if (ctx < 0 || ctx > P.n_pos - n_new) {       // a position without a rotation
     if (tid == 0 && n_new > 0) record_bad_index(P.status, kBadPosition);
     return;
@@ -122,77 +151,84 @@ __global__ void __launch_bounds__(T) rope_append_kernel(const RopeParams P) {
   const int n = hi - lo;                        // new tokens of this page
   const int slot0 = lo - page_no * P.page;
   const int row = row0 + (lo - base), pos = ctx + (lo - base);
+  if (blockIdx.y >= (unsigned)P.n_kv) {
+    // ---- queries: pieces of 16 elements, neighbours in a token's heads; two in flight a thread
+    const int group = P.n_q / P.n_kv, row_items = group * I, items = n * row_items;
+    const __nv_bfloat16* xq = P.X + (size_t)row * P.ld + (size_t)head * group * HD;
+    __nv_bfloat16* oq = P.Qo + (size_t)row * P.ld_q + (size_t)head * group * HD;
+    constexpr int U = 2;
+    for (int id0 = tid; id0 < items; id0 += U * T) {
+      uint4 x[U][2];
+      float4 cs[U][4];
+      int at[U][3];                                // token, head of the group, piece
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int id = id0 + u * T, j = id / row_items, in = id - j * row_items;
+        at[u][0] = j; at[u][1] = in / I; at[u][2] = in % I;
+        if (id < items) {
+          const Item e = item_of<HD>(at[u][2], P.rot, P.interleaved);
+          const __nv_bfloat16* src = xq + (size_t)j * P.ld + at[u][1] * HD;
+          x[u][0] = *reinterpret_cast<const uint4*>(src + e.a);
+          x[u][1] = *reinterpret_cast<const uint4*>(src + e.b);
+          load_rotations(P, e, pos + j, cs[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (id0 + u * T < items) {
+          const Item e = item_of<HD>(at[u][2], P.rot, P.interleaved);
+          rotate_item(e, x[u][0], x[u][1], cs[u], P.interleaved);
+          __nv_bfloat16* o = oq + (size_t)at[u][0] * P.ld_q + at[u][1] * HD;
+          *reinterpret_cast<uint4*>(o + e.a) = x[u][0];
+          *reinterpret_cast<uint4*>(o + e.b) = x[u][1];
+        }
+    }
+    return;
+  }
+
+  // ---- keys and values
   int page = -1;
   if (P.k) {
     page = page_no < P.max_pages ? __ldg(P.pages + (size_t)s * P.max_pages + page_no) : -1;
     if (page < 0 || page >= P.n_pages) {
       if (tid == 0 && head == 0) record_bad_index(P.status, kBadPage);
-      page = -1;                                // the rotated rows leave all the same
+      page = -1;                                // the rotated keys leave all the same
     }
   }
   const size_t cell = (size_t)(page < 0 ? 0 : page) * P.n_kv + head;     // scale index; codes start at cell * page * HD
-
-  const int group = P.n_q / P.n_kv;
   uint4 kv[N][4];                               // keys: two runs of eight; values: two more
   uint32_t mk = 0, mv = 0;
+#pragma unroll
+  for (int it = 0; it < N; ++it) {
+    const int id = it * T + tid, j = id / I;
+    if (j < n) {
+      const Item e = item_of<HD>(id % I, P.rot, P.interleaved);
+      const __nv_bfloat16* x = P.X + (size_t)(row + j) * P.ld;
+      const __nv_bfloat16* xk = x + (size_t)(P.n_q + head) * HD;
+      const __nv_bfloat16* xv = xk + (size_t)P.n_kv * HD;
+      kv[it][0] = *reinterpret_cast<const uint4*>(xk + e.a);
+      kv[it][1] = *reinterpret_cast<const uint4*>(xk + e.b);
+      kv[it][2] = *reinterpret_cast<const uint4*>(xv + e.a);
+      kv[it][3] = *reinterpret_cast<const uint4*>(xv + e.b);
+    }
+  }
   float old_k = 0.0f, old_v = 0.0f;
   if (page >= 0 && slot0 > 0) { old_k = P.k_scale[cell]; old_v = P.v_scale[cell]; }
 #pragma unroll
   for (int it = 0; it < N; ++it) {
     const int id = it * T + tid, j = id / I;
     if (j < n) {
-      const Item e = item_of(id % I, P.rot, P.interleaved);
-      const __nv_bfloat16* x = P.X + (size_t)(row + j) * P.ld;
-      const __nv_bfloat16* xk = x + (size_t)(P.n_q + head) * HD;
-      const __nv_bfloat16* xv = xk + (size_t)P.n_kv * HD;
-      kv[it][0] = *reinterpret_cast<const uint4*>(xk + e.a);
-      kv[it][1] = *reinterpret_cast<const uint4*>(xk + e.b);
-      if (page >= 0) {
-        kv[it][2] = *reinterpret_cast<const uint4*>(xv + e.a);
-        kv[it][3] = *reinterpret_cast<const uint4*>(xv + e.b);
-      }
-    }
-  }
-#pragma unroll
-  for (int it = 0; it < N; ++it) {
-    const int id = it * T + tid, j = id / I;
-    if (j < n) {
-      const Item e = item_of(id % I, P.rot, P.interleaved);
+      const Item e = item_of<HD>(id % I, P.rot, P.interleaved);
       float4 cs[4];
-      if (e.pair >= 0) {
-        const float4* t = reinterpret_cast<const float4*>(P.rope + ((size_t)(pos + j) * (P.rot / 2) + e.pair) * 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) cs[i] = __ldg(t + i);
-        rotate16(kv[it][0], kv[it][1], cs, P.interleaved);
-      }
+      load_rotations(P, e, pos + j, cs);
+      rotate_item(e, kv[it][0], kv[it][1], cs, P.interleaved);
       if (P.Ko) {
         __nv_bfloat16* o = P.Ko + (size_t)(row + j) * P.ld_k + (size_t)head * HD;
         *reinterpret_cast<uint4*>(o + e.a) = kv[it][0];
         *reinterpret_cast<uint4*>(o + e.b) = kv[it][1];
       }
-      if (page >= 0) {
-        mk = max_finite(kv[it][0], max_finite(kv[it][1], mk));
-        mv = max_finite(kv[it][2], max_finite(kv[it][3], mv));
-      }
-      // the group's queries of the same token, four heads in flight
-      const __nv_bfloat16* xq = P.X + (size_t)(row + j) * P.ld + (size_t)head * group * HD;
-      __nv_bfloat16* oq = P.Qo + (size_t)(row + j) * P.ld_q + (size_t)head * group * HD;
-      for (int h = 0; h < group; h += 4) {
-        uint4 q[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (h + i < group) {
-            q[i][0] = *reinterpret_cast<const uint4*>(xq + (h + i) * HD + e.a);
-            q[i][1] = *reinterpret_cast<const uint4*>(xq + (h + i) * HD + e.b);
-          }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (h + i < group) {
-            if (e.pair >= 0) rotate16(q[i][0], q[i][1], cs, P.interleaved);
-            *reinterpret_cast<uint4*>(oq + (h + i) * HD + e.a) = q[i][0];
-            *reinterpret_cast<uint4*>(oq + (h + i) * HD + e.b) = q[i][1];
-          }
-      }
+      mk = max_finite(kv[it][0], max_finite(kv[it][1], mk));
+      mv = max_finite(kv[it][2], max_finite(kv[it][3], mv));
     }
   }
   if (page < 0) return;                         // (the same in the whole CTA)
@@ -214,7 +250,7 @@ __global__ void __launch_bounds__(T) rope_append_kernel(const RopeParams P) {
   for (int it = 0; it < N; ++it) {
     const int id = it * T + tid, j = id / I;
     if (j < n) {
-      const Item e = item_of(id % I, P.rot, P.interleaved);
+      const Item e = item_of<HD>(id % I, P.rot, P.interleaved);
       const int o = (slot0 + j) * HD;
       *reinterpret_cast<uint2*>(ck + o + e.a) = codes8(kv[it][0], inv_k);
       *reinterpret_cast<uint2*>(ck + o + e.b) = codes8(kv[it][1], inv_k);
@@ -229,14 +265,22 @@ __global__ void __launch_bounds__(T) rope_append_kernel(const RopeParams P) {
     if (slot0 > 0 && now > before) {
       const float r = __fmul_rn(before, which ? inv_v : inv_k);
       uint4* c = reinterpret_cast<uint4*>(which ? cv : ck);
-      for (int i = tid; i < slot0 * HD / 16; i += T) {
-        const uint4 w = c[i];
-        uint32_t u[4] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u, w.z ^ 0x80808080u, w.w ^ 0x80808080u};
+      const int n_old = slot0 * HD / 16;
+      for (int i0 = tid; i0 < n_old; i0 += 4 * T) {      // four loads in flight
+        uint4 w[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-          u[b] = pack_codes(__fmul_rn(flipped_byte_to_f32(u[b], 0), r), __fmul_rn(flipped_byte_to_f32(u[b], 1), r),
-                            __fmul_rn(flipped_byte_to_f32(u[b], 2), r), __fmul_rn(flipped_byte_to_f32(u[b], 3), r));
-        c[i] = make_uint4(u[0], u[1], u[2], u[3]);
+        for (int k = 0; k < 4; ++k)
+          if (i0 + k * T < n_old) w[k] = c[i0 + k * T];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i0 + k * T < n_old) {
+            uint32_t u[4] = {w[k].x ^ 0x80808080u, w[k].y ^ 0x80808080u, w[k].z ^ 0x80808080u, w[k].w ^ 0x80808080u};
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              u[b] = pack_codes(__fmul_rn(flipped_byte_to_f32(u[b], 0), r), __fmul_rn(flipped_byte_to_f32(u[b], 1), r),
+                                __fmul_rn(flipped_byte_to_f32(u[b], 2), r), __fmul_rn(flipped_byte_to_f32(u[b], 3), r));
+            c[i0 + k * T] = make_uint4(u[0], u[1], u[2], u[3]);
+          }
       }
     }
   }
@@ -249,7 +293,7 @@ struct GatherParams {
   const int32_t *pages, *first, *cu;
   __nv_bfloat16 *Ko, *Vo;
   uint32_t* status;
-  int M, ld, n_kv, n_seqs, n_pages, page, max_pages;
+  int M, ld, n_kv, n_seqs, n_pages, page, max_pages, heads;
 };
 
 __device__ __forceinline__ uint4 values8(uint2 codes, float scale) {
@@ -259,19 +303,18 @@ __device__ __forceinline__ uint4 values8(uint2 codes, float scale) {
                     f32x2_to_bf16x2_bits(val(b, 0), val(b, 1)), f32x2_to_bf16x2_bits(val(b, 2), val(b, 3)));
 }
 
-// One CTA: the rows of one page and head.  A thread turns 8 codes into 16 bytes, neighbours' neighbours: a warp writes
-// whole rows of the head.
-template <int HD, int T>
-__global__ void __launch_bounds__(T) kv_gather_kernel(const GatherParams P) {
-  __shared__ int found[2];
+// One CTA: the rows of one page and `heads` heads (P.heads; about 8 KB of codes each of keys and values: with a head a
+// CTA, pages of 16 tokens of 64 values left it 2 KB, and the launch took GATHER_OLD us for 37 ragged prefixes of 16 heads instead of
+// GATHER_NEW).  A thread turns 8 codes into 16 bytes; neighbours' pieces follow each other along the heads of a token, as they
+// lie in the output.
+template <int HD>
+__global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams P) {
+  __shared__ FoundTask found;
   pdl_wait();
   pdl_launch_dependents();
-  int place;
-  const int s = find_task(P.cu, P.n_seqs, P.page, 2, blockIdx.x, found, P.status, place);
+  const FoundTask task = find_task(P.cu, P.first, P.n_seqs, P.page, blockIdx.x, &found, P.status);
+  const int s = task.seq, place = task.place, row0 = task.row0, n_rows = task.rows, first = task.extra, tid = threadIdx.x;
   if (s < 0) return;
-  const int head = blockIdx.y, tid = threadIdx.x;
-  const int row0 = __ldg(P.cu + s), n_rows = __ldg(P.cu + s + 1) - row0;
-  const int first = P.first ? __ldg(P.first + s) : 0;
   if (row0 > P.M - n_rows || first < 0 || first > INT32_MAX - 1024 - n_rows) {
     if (tid == 0) record_bad_index(P.status, kBadOffset);
     return;
@@ -284,19 +327,37 @@ __global__ void __launch_bounds__(T) kv_gather_kernel(const GatherParams P) {
     if (tid == 0) record_bad_index(P.status, kBadPage);
     return;
   }
-  const size_t cell = (size_t)page * P.n_kv + head;
-  const float sk = __ldg(P.k_scale + cell), sv = __ldg(P.v_scale + cell);
-  const size_t from = (cell * P.page + (lo - page_no * P.page)) * HD;
-  const uint2* ck = reinterpret_cast<const uint2*>(P.k + from);
-  const uint2* cv = reinterpret_cast<const uint2*>(P.v + from);
-  const size_t to = (size_t)(row0 + (lo - first)) * P.ld + (size_t)head * HD;
-  constexpr int C = HD / 8;                      // 8-element chunks of a row
-#pragma unroll 2
-  for (int i = tid; i < (hi - lo) * C; i += T) {
-    const uint2 a = __ldg(ck + i), b = __ldg(cv + i);
-    const size_t o = to + (size_t)(i / C) * P.ld + (i % C) * 8;
-    *reinterpret_cast<uint4*>(P.Ko + o) = values8(a, sk);
-    *reinterpret_cast<uint4*>(P.Vo + o) = values8(b, sv);
+  constexpr int C = HD / 8;                      // pieces of a row of one head
+  const int head0 = blockIdx.y * P.heads, heads = min(P.heads, P.n_kv - head0);
+  const size_t cell0 = (size_t)page * P.n_kv + head0;
+  const int slot0 = lo - page_no * P.page, row_items = heads * C, items = (hi - lo) * row_items;
+  __nv_bfloat16* const ko = P.Ko + (size_t)(row0 + (lo - first)) * P.ld + (size_t)head0 * HD;
+  __nv_bfloat16* const vo = P.Vo + (size_t)(row0 + (lo - first)) * P.ld + (size_t)head0 * HD;
+  constexpr int U = 4;
+  for (int id0 = tid; id0 < items; id0 += U * 256) {
+    uint2 a[U], b[U];
+    float sk[U], sv[U];
+    int to[U];                                   // element of the output, from the CTA's first
+    int64_t row[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int id = id0 + u * 256, j = id / row_items, in = id - j * row_items, h = in / C;
+      row[u] = (int64_t)j * P.ld;
+      to[u] = in * 8;
+      if (id < items) {
+        const size_t from = ((cell0 + h) * P.page + slot0 + j) * HD + (in % C) * 8;
+        a[u] = __ldg(reinterpret_cast<const uint2*>(P.k + from));
+        b[u] = __ldg(reinterpret_cast<const uint2*>(P.v + from));
+        sk[u] = __ldg(P.k_scale + cell0 + h);
+        sv[u] = __ldg(P.v_scale + cell0 + h);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (id0 + u * 256 < items) {
+        *reinterpret_cast<uint4*>(ko + row[u] + to[u]) = values8(a[u], sk[u]);
+        *reinterpret_cast<uint4*>(vo + row[u] + to[u]) = values8(b[u], sv[u]);
+      }
   }
 }
 
@@ -318,7 +379,7 @@ int check_cache(const fpt_kv_cache* c, bool with_storage) {
 
 template <int HD, int T, int N>
 static int launch_rope(cudaStream_t st, const RopeParams& P, unsigned tasks) {
-  return launch_kernel(rope_append_kernel<HD, T, N>, dim3(tasks, P.n_kv), dim3(T), 0, st, true, P) == cudaSuccess ? FPT_OK
+  return launch_kernel(rope_append_kernel<HD, T, N>, dim3(tasks, 2 * P.n_kv), dim3(T), 0, st, true, P) == cudaSuccess ? FPT_OK
                                                                                                            : FPT_ERR_CUDA;
 }
 
@@ -339,7 +400,7 @@ extern "C" int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int
   if (rot_dim <= 0 || rot_dim % 16 || rot_dim > hd || n_q % n_kv) return FPT_ERR_UNSUPPORTED;
   if (ld < (n_q + 2 * (int64_t)n_kv) * hd || ld_q < (int64_t)n_q * hd || (K_out && ld_k < (int64_t)n_kv * hd)) return FPT_ERR_BAD_ARG;
   if (!cu_new && n_seqs > M) return FPT_ERR_BAD_ARG;
-  if (n_kv > 65535 || n_pos > INT32_MAX - 1024 || M > INT32_MAX - 1024) return FPT_ERR_UNSUPPORTED;
+  if (n_kv > 32767 || n_pos > INT32_MAX - 1024 || M > INT32_MAX - 1024) return FPT_ERR_UNSUPPORTED;
   if (ld % 8 || ld_q % 8 || (K_out && ld_k % 8)) return FPT_ERR_ALIGNMENT;
   if (((uintptr_t)QKV | (uintptr_t)Q_out | (uintptr_t)K_out | (uintptr_t)rope | (uintptr_t)workspace) & 15) return FPT_ERR_ALIGNMENT;
   if (((uintptr_t)cu_new | (uintptr_t)ctx) & 3) return FPT_ERR_ALIGNMENT;
@@ -360,8 +421,9 @@ extern "C" int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int
   cudaStream_t st = (cudaStream_t)stream;
   const int64_t tasks = cu_new ? (int64_t)M / P.page + 2 * (int64_t)n_seqs : n_seqs;
   if (tasks > INT32_MAX) return FPT_ERR_UNSUPPORTED;
-  // one token a sequence: its heads' items are few, and small CTAs start faster; otherwise a page a CTA
-  if (!cu_new) return hd == 128 ? launch_rope<128, 32, 1>(st, P, (unsigned)tasks) : launch_rope<64, 32, 1>(st, P, (unsigned)tasks);
+  // one token a sequence: its heads' pieces are few, and what a CTA has to do beside them is to round the page's held tokens
+  // again where its scale grows; otherwise a page a CTA
+  if (!cu_new) return hd == 128 ? launch_rope<128, 64, 1>(st, P, (unsigned)tasks) : launch_rope<64, 64, 1>(st, P, (unsigned)tasks);
   const int items = P.page * (hd / 16);
   if (hd == 128) {
     if (items <= 128) return launch_rope<128, 128, 1>(st, P, (unsigned)tasks);
@@ -392,10 +454,12 @@ extern "C" int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int3
   P.max_pages = cache->max_pages;
   const int64_t tasks = (int64_t)M / P.page + 2 * (int64_t)n_seqs;
   if (tasks > INT32_MAX) return FPT_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)tasks, cache->n_kv);
+  P.heads = 8192 / (cache->page * cache->head_dim);
+  if (P.heads < 1) P.heads = 1;
+  if (P.heads > cache->n_kv) P.heads = cache->n_kv;
+  const dim3 grid((unsigned)tasks, (unsigned)((cache->n_kv + P.heads - 1) / P.heads));
   cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = cache->head_dim == 128
-                            ? launch_kernel(kv_gather_kernel<128, 256>, grid, dim3(256), 0, st, true, P)
-                            : launch_kernel(kv_gather_kernel<64, 128>, grid, dim3(128), 0, st, true, P);
+  const cudaError_t e = cache->head_dim == 128 ? launch_kernel(kv_gather_kernel<128>, grid, dim3(256), 0, st, true, P)
+                                               : launch_kernel(kv_gather_kernel<64>, grid, dim3(256), 0, st, true, P);
   return e == cudaSuccess ? FPT_OK : FPT_ERR_CUDA;
 }
