@@ -592,11 +592,21 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             float top = -INFINITY;
             // (a batch of loads has a fixed length, what lies behind the last part left out: the tail of an unrolled loop would
             // wait for one load after the other, 6 us of 11 with 55 parts)
-            for (int p = p0; p < nparts; p += 4 * kStep) {
-              float m[4];
+            float m0[4], l0[4];                         // the first batch stays
+            auto load = [&](int from, int until, float (&m)[4], float (&l)[4]) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                m[k] = p + k * kStep < nparts && h0 < gh ? __ldcg(part_at(p + k * kStep) + NH * HD + h0) : -INFINITY;
+              for (int k = 0; k < 4; ++k) {
+                const bool there = from + k * kStep < until && h0 < gh;
+                const float* w = part_at(there ? from + k * kStep : 0) + NH * HD;
+                m[k] = there ? __ldcg(w + h0) : -INFINITY;
+                l[k] = there ? __ldcg(w + NH + h0) : 0.0f;
+              }
+            };
+            load(p0, nparts, m0, l0);
+            top = fmaxf(fmaxf(m0[0], m0[1]), fmaxf(m0[2], m0[3]));
+            for (int p = p0 + 4 * kStep; p < nparts; p += 4 * kStep) {
+              float m[4], l[4];
+              load(p, nparts, m, l);
               top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
             }
             merge[tid] = top;
@@ -613,14 +623,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             for (int from = 0; from < nparts; from += kRoom) {
               const int n_here = min(kRoom, nparts - from);
               for (int p = p0; p < n_here; p += 4 * kStep) {
-                float m[4], l[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const bool there = p + k * kStep < n_here && h0 < gh;
-                  const float* w = part_at(from + (there ? p + k * kStep : 0)) + NH * HD;
-                  m[k] = there ? __ldcg(w + h0) : -INFINITY;
-                  l[k] = there ? __ldcg(w + NH + h0) : 0.0f;
-                }
+                float m[4] = {m0[0], m0[1], m0[2], m0[3]}, l[4] = {l0[0], l0[1], l0[2], l0[3]};
+                if (from + p != p0) load(from + p, from + n_here, m, l);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                   const float r = m[k] == -INFINITY ? 0.0f : ex2(m[k] - top);
@@ -667,6 +671,16 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           }
         }
         if (!meet()) break;                           // the buffers are free for the next row
+        // (the next tile begins a row; said here, so that nothing of this one is kept in registers through the join)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          M[t][0] = M[t][1] = l[t][0] = l[t][1] = qscale[t][0] = qscale[t][1] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            qf[t][k][0] = qf[t][k][1] = 0;
+            O[t][k][0] = O[t][k][1] = O[t][k][2] = O[t][k][3] = 0.0f;
+          }
+        }
       }
     }
   }
