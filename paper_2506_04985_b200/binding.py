@@ -47,7 +47,7 @@ class _KVCacheStruct(ctypes.Structure):
 class KVCache:
     """A paged 8-bit cache (see `fpt_kv_cache`): codes int8 [n_pages, n_kv, page, head_dim], scales f32 [n_pages, n_kv],
     page table int32 [n_seqs, max_pages], all contiguous on one device."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "struct", "ref")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "dev", "struct", "ref")
 
     def __init__(self, k, v, k_scale, v_scale, pages):
         shape = k.shape
@@ -58,7 +58,9 @@ class KVCache:
                 v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous() and pages.is_contiguous()):
             raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table are wanted")
         self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
-        self.n_kv, self.head_dim = n_kv, hd
+        self.n_kv, self.head_dim, self.dev = n_kv, hd, k.get_device()
+        if not (self.dev == v.get_device() == k_scale.get_device() == v_scale.get_device() == pages.get_device()):
+            raise ValueError("KVCache: tensors of one device are wanted")
         self.n_seqs, max_pages = pages.shape
         self.struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages.data_ptr(),
                                      n_pages, n_kv, page, hd, max_pages)
@@ -69,7 +71,7 @@ class KVCache:
         """Stands for no storage: fpt_rope_append then only rotates."""
         c = cls.__new__(cls)
         c.k = c.v = c.k_scale = c.v_scale = c.pages = None
-        c.n_seqs, c.n_kv, c.head_dim = 0, n_kv, head_dim
+        c.n_seqs, c.n_kv, c.head_dim, c.dev = 0, n_kv, head_dim, -1
         c.struct = _KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0)
         c.ref = ctypes.byref(c.struct)
         return c
@@ -359,20 +361,31 @@ def _bad(where):
     return FptError(ERR_BAD_ARG, where)
 
 
-def _rows(t, where):
-    """Leading dimension of a bf16 [rows, columns] tensor whose rows are contiguous."""
+def _rows(t, dev, where):
+    """Leading dimension of a bf16 [rows, columns] tensor on device `dev` whose rows are contiguous."""
     strides = t.stride()
-    if t.dtype is not torch.bfloat16 or len(strides) != 2 or strides[1] != 1:
+    if t.dtype is not torch.bfloat16 or len(strides) != 2 or strides[1] != 1 or t.get_device() != dev:
         raise _bad(where)
     ld, (rows, cols) = strides[0], t.shape
     return ld if rows > 1 or ld >= cols else cols
 
 
-def _i32(t, n, where):
-    """Address of an int32 [n] tensor."""
-    if t.dtype is not torch.int32 or t.shape != (n,) or (n > 1 and t.stride() != (1,)):
+def _i32(t, n, dev, where):
+    """Address of an int32 [n] tensor on device `dev`."""
+    if t.dtype is not torch.int32 or t.shape != (n,) or (n > 1 and t.stride() != (1,)) or t.get_device() != dev:
         raise _bad(where)
     return t.data_ptr()
+
+
+def _scratch(ws, dev, where):
+    """Address and size of a workspace on device `dev`, which has to be the current one (a new workspace for None)."""
+    if dev != (_device() if _device is not None else torch.cuda.current_device()):
+        raise _bad(where)
+    if ws is None:
+        ws = new_workspace(OP_ATTN, 1, 1, 1, torch.device("cuda", dev))
+    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise _bad(where)
+    return ws.data_ptr(), ws.numel()
 
 
 def _like(t):
@@ -391,8 +404,10 @@ def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, w
     M, cols = QKV.shape
     hd, n_kv, n = cache.head_dim, cache.n_kv, ctx.shape[0]
     n_pos, pairs, two = rope.shape
-    if (rope.dtype is not torch.float32 or two != 2 or not rope.is_contiguous() or cols < (n_q + 2 * n_kv) * hd or
-            (cache.pages is not None and cache.n_seqs < n)):
+    dev = QKV.get_device()
+    scratch = _scratch(ws, dev, where)
+    if (rope.dtype is not torch.float32 or two != 2 or not rope.is_contiguous() or rope.get_device() != dev or
+            cols < (n_q + 2 * n_kv) * hd or (cache.pages is not None and (cache.n_seqs < n or cache.dev != dev))):
         raise _bad(where)
     if Q is None:
         Q = _new(QKV, (M, n_q * hd), torch.bfloat16)
@@ -403,12 +418,10 @@ def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, w
             K = _new(QKV, (M, n_kv * hd), torch.bfloat16)
     elif K.shape != (M, n_kv * hd):
         raise _bad(where)
-    if ws is None:
-        ws = new_workspace(OP_ATTN, 1, 1, 1, QKV.device)
-    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, _rows(QKV, where), n_q, rope.data_ptr(), n_pos, 2 * pairs, layout,
-                                 None if cu_new is None else _i32(cu_new, n + 1, where), _i32(ctx, n, where), n, cache.ref,
-                                 Q.data_ptr(), _rows(Q, where), None if K is None else K.data_ptr(),
-                                 0 if K is None else _rows(K, where), ws.data_ptr(), ws.numel()), where)
+    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, _rows(QKV, dev, where), n_q, rope.data_ptr(), n_pos, 2 * pairs, layout,
+                                 None if cu_new is None else _i32(cu_new, n + 1, dev, where), _i32(ctx, n, dev, where), n, cache.ref,
+                                 Q.data_ptr(), _rows(Q, dev, where), None if K is None else K.data_ptr(),
+                                 0 if K is None else _rows(K, dev, where), *scratch), where)
     return Q, K
 
 
@@ -416,19 +429,19 @@ def fpt_kv_gather(cache, cu_out, M, first=None, K=None, V=None, ws=None):
     """Cached tokens first[s] ... of every sequence in bf16 -> (K, V) [M, n_kv head_dim], packed by cu_out int32 [n_seqs + 1]."""
     where = "fpt_kv_gather"
     n, shape = cu_out.shape[0] - 1, (M, cache.n_kv * cache.head_dim)
+    dev = cache.dev
     if cache.pages is None or cache.n_seqs < n:
         raise _bad(where)
+    scratch = _scratch(ws, dev, where)
     if K is None:
         K = _new(cu_out, shape, torch.bfloat16)
     if V is None:
         V = _like(K) if K.is_contiguous() else _new(cu_out, shape, torch.bfloat16)
-    if ws is None:
-        ws = new_workspace(OP_ATTN, 1, 1, 1, cu_out.device)
-    ld = _rows(K, where)
-    if _rows(V, where) != ld or K.shape != shape or V.shape != shape:
+    ld = _rows(K, dev, where)
+    if _rows(V, dev, where) != ld or K.shape != shape or V.shape != shape:
         raise _bad(where)
-    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, where), _i32(cu_out, n + 1, where),
-                               n, M, K.data_ptr(), V.data_ptr(), ld, ws.data_ptr(), ws.numel()), where)
+    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, dev, where),
+                               _i32(cu_out, n + 1, dev, where), n, M, K.data_ptr(), V.data_ptr(), ld, *scratch), where)
     return K, V
 
 
@@ -438,18 +451,18 @@ def fpt_attn_decode(Q, cache, kv_len, scale=None, want_lse=False, O=None, ws=Non
     n, cols = shape = Q.shape
     hd = cache.head_dim
     n_q = cols // hd
+    dev = cache.dev
     if cache.n_seqs < n or cols != n_q * hd:
         raise _bad(where)
+    scratch = _scratch(ws, dev, where)
     if O is None:
         O = _like(Q)
     elif O.shape != shape:
         raise _bad(where)
     lse = _new(Q, (n, n_q), torch.float32) if want_lse else None
-    if ws is None:
-        ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
-    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, where), n_q, cache.ref, _i32(kv_len, n, where), n,
-                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, where),
-                                 None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel()), where)
+    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, dev, where), n_q, cache.ref, _i32(kv_len, n, dev, where), n,
+                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, dev, where),
+                                 None if lse is None else lse.data_ptr(), *scratch), where)
     return O, lse
 
 
@@ -459,7 +472,8 @@ def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None
     where = "fpt_attn_prompt"
     Mq, cols = shape = Q.shape
     Mk, cols_k = K.shape
-    hd, n = cols // n_q, cu_q.shape[0] - 1
+    hd, n, dev = cols // max(n_q, 1), cu_q.shape[0] - 1, Q.get_device()
+    scratch = _scratch(ws, dev, where)
     if cols != n_q * hd or cols_k != n_kv * hd or V.shape != K.shape:
         raise _bad(where)
     if O is None:
@@ -467,13 +481,11 @@ def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None
     elif O.shape != shape:
         raise _bad(where)
     lse = _new(Q, (Mq, n_q), torch.float32) if want_lse else None
-    if ws is None:
-        ws = new_workspace(OP_ATTN, 1, 1, 1, Q.device)
-    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, where), Mq, K.data_ptr(), _rows(K, where), V.data_ptr(),
-                                 _rows(V, where), Mk, n_q, n_kv, hd, _i32(cu_q, n + 1, where),
-                                 None if cu_k is None else _i32(cu_k, n + 1, where), n, int(bool(causal)),
-                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, where),
-                                 None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel()), where)
+    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, dev, where), Mq, K.data_ptr(), _rows(K, dev, where),
+                                 V.data_ptr(), _rows(V, dev, where), Mk, n_q, n_kv, hd, _i32(cu_q, n + 1, dev, where),
+                                 None if cu_k is None else _i32(cu_k, n + 1, dev, where), n, int(bool(causal)),
+                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, dev, where),
+                                 None if lse is None else lse.data_ptr(), *scratch), where)
     return O, lse
 
 

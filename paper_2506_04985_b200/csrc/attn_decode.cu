@@ -704,6 +704,11 @@ static int launch_decode(cudaStream_t st, const fpt_kv_cache* c, DecodeParams P)
   using L = DecSmem<HD, NT, ST>;
   static_assert((L::kAlloc + 1024) * MINB <= 228 * 1024, "the ring does not fit");
   static_assert(ST <= 8, "a batch of tiles has to be longer than the ring");
+  P.blocks = (P.group + 8 * NT - 1) / (8 * NT);
+  // a CTA for each tile at most; tiles are counted in 32 bits
+  const int64_t rows_of_heads = (int64_t)P.n_seqs * P.n_kv * P.blocks, longest = ((int64_t)c->max_pages * c->page + kDecTile - 1) / kDecTile;
+  if (rows_of_heads > INT32_MAX / longest) return FPT_ERR_UNSUPPORTED;
+  const int64_t most = rows_of_heads * longest;
   auto kern = attn_decode_kernel<HD, NT, ST, MINB>;
   static PerDeviceInt attr_set;
   if (!ensure_smem_attr(attr_set, kern, L::kAlloc)) return FPT_ERR_CUDA;
@@ -711,10 +716,6 @@ static int launch_decode(cudaStream_t st, const fpt_kv_cache* c, DecodeParams P)
   const int64_t rows = (int64_t)c->n_pages * c->n_kv * c->page;
   const int box = c->page < kDecTile ? c->page : kDecTile;
   if (!make_code_map(&tmK, c->k, rows, HD, box) || !make_code_map(&tmV, c->v, rows, HD, box)) return FPT_ERR_CUDA;
-  P.blocks = (P.group + 8 * NT - 1) / (8 * NT);
-  // a CTA for each tile at most
-  const int64_t most = (int64_t)P.n_seqs * P.n_kv * P.blocks * (((int64_t)c->max_pages * c->page + kDecTile - 1) / kDecTile);
-  if (most > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   int64_t grid = (int64_t)device_sm_count() * MINB;
   if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
   if (grid > most) grid = most;
@@ -751,13 +752,9 @@ extern "C" int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, c
   while ((1 << P.page_log2) < P.page) ++P.page_log2;
   P.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)stream;
-#ifndef DEC_CFG
-#define DEC_CFG 128, 1, 3, 3
-#endif
-#ifndef DEC_CFG64
-#define DEC_CFG64 64, 1, 6, 3
-#endif
+  // Three CTAs an SM where registers and shared memory allow it: with two, and as much in flight, a tile in each takes its time
+  // (131071 tokens of 8 heads: 57 and 64 us, 64 ragged sequences: 136 and 161).
   if (cache->head_dim == 128)
-    return P.group <= 8 ? launch_decode<DEC_CFG>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
-  return P.group <= 8 ? launch_decode<DEC_CFG64>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);
+    return P.group <= 8 ? launch_decode<128, 1, 3, 3>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
+  return P.group <= 8 ? launch_decode<64, 1, 6, 3>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);
 }

@@ -32,6 +32,7 @@ constexpr int kPrThreads = 512;
 constexpr int kPrSoftRegs = 176, kPrEndRegs = 80, kPrAuxRegs = 80;
 static_assert(128 * (2 * kPrSoftRegs + kPrEndRegs + kPrAuxRegs) <= kPrThreads * 128, "the warpgroups' registers exceed the launch's");
 constexpr int kPrEarly = 6;                // of the eight 16-key steps of P V, those that begin before the last weights are there
+static_assert(kPrEarly % 2 == 0 && kPrEarly < 8, "weights leave two steps at a time");
 
 // Lane l of four: y[i] becomes y[l & 3] of lane (l & ~3) + i.  (Written out: an index that the compiler does not see through
 // would put y into local memory, and with 227 KB of shared memory there is hardly a cache behind it.)
@@ -179,37 +180,68 @@ __device__ __forceinline__ int block_of_answer(uint32_t answer) {
   return x;
 }
 
-// Up to 32 sequences are taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short:
-// lane s knows where the tasks of sequence s begin and how many they are.
-struct TaskOrder { int first, count; };
+// Where the tasks of up to 128 sequences begin and how many they are: lane l knows it of sequences l, l + 32, ...  Up to 32 are
+// taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short; more as they come.
+constexpr int kPrHeld = 4;
+struct TaskOrder { int first[kPrHeld], count[kPrHeld]; };
 __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane) {
-  TaskOrder o = {0, 0};
-  if (P.n_seqs > 32) return o;
-  int keys = -1;
-  if (lane < P.n_seqs) {
-    const int len_q = __ldg(P.cu_q + lane + 1) - __ldg(P.cu_q + lane), len_k = __ldg(P.cu_k + lane + 1) - __ldg(P.cu_k + lane);
-    o.count = max(0, len_q + ((256 >> P.pack_log2) - 1)) >> (8 - P.pack_log2);
-    keys = max(0, len_k);
-  }
-  for (int s = 0; s < P.n_seqs; ++s) {
-    const int k = __shfl_sync(0xffffffffu, keys, s), c = __shfl_sync(0xffffffffu, o.count, s);
-    if (k > keys || (k == keys && s < lane)) o.first += c;
+  TaskOrder o;
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kPrHeld; ++i) {
+    o.first[i] = 0;
+    o.count[i] = 0;
+    const int s = lane + 32 * i;
+    if (P.n_seqs > 32 * kPrHeld || 32 * i >= P.n_seqs) continue;
+    int keys = -1;
+    if (s < P.n_seqs) {
+      const int q0 = __ldg(P.cu_q + s), q1 = __ldg(P.cu_q + s + 1), k0 = __ldg(P.cu_k + s), k1 = __ldg(P.cu_k + s + 1);
+      if (q0 < 0 || q1 < q0 || q1 > P.M_q || k0 < 0 || k1 < k0 || k1 > P.M_k) {
+        record_bad_index(P.status, kBadOffset);
+      } else {
+        keys = k1 - k0;
+        o.count[i] = (q1 - q0 + ((256 >> P.pack_log2) - 1)) >> (8 - P.pack_log2);
+      }
+    }
+    if (P.n_seqs <= 32) {
+      for (int k = 0; k < P.n_seqs; ++k) {
+        const int other = __shfl_sync(0xffffffffu, keys, k), c = __shfl_sync(0xffffffffu, o.count[i], k);
+        if (other > keys || (other == keys && k < lane)) o.first[i] += c;
+      }
+    } else {
+      int v = o.count[i];
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, v, k);
+        if (lane >= k) v += u;
+      }
+      o.first[i] = before + v - o.count[i];
+      before += __shfl_sync(0xffffffffu, v, 31);
+    }
   }
   return o;
 }
 
-// The task of block `bid`; whole warp, the same answer in every lane.  With more sequences than lanes, sequence s has
+// The task of block `bid`; whole warp, the same answer in every lane.  With more sequences than are held, sequence s has
 // floor(cu_q[s+1] / per) - floor(cu_q[s] / per) + 1 tasks (at least the blocks of `per` rows that it needs), and which s a task belongs to
 // is found 32 places at a time.
 __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const TaskOrder& order, int bid, int lane, TaskInfo& ti) {
   const int per_log2 = 8 - P.pack_log2, per = 1 << per_log2;
   const int turn = bid / P.units, unit = bid - turn * P.units;
   int lo = 0, place;
-  if (P.n_seqs <= 32) {
-    const uint32_t mine = __ballot_sync(0xffffffffu, turn >= order.first && turn < order.first + order.count);
-    if (mine == 0) return false;
-    lo = __ffs(mine) - 1;
-    place = __shfl_sync(0xffffffffu, order.first + order.count, lo) - 1 - turn;      // last rows first
+  if (P.n_seqs <= 32 * kPrHeld) {
+    lo = -1;
+    place = 0;
+#pragma unroll
+    for (int i = 0; i < kPrHeld; ++i) {
+      const uint32_t mine = __ballot_sync(0xffffffffu, turn >= order.first[i] && turn < order.first[i] + order.count[i]);
+      if (mine) {
+        const int l = __ffs(mine) - 1;
+        lo = l + 32 * i;
+        place = __shfl_sync(0xffffffffu, order.first[i] + order.count[i], l) - 1 - turn;      // last rows first
+      }
+    }
+    if (lo < 0) return false;
   } else {
     const int id = P.n_tasks - 1 - turn;
     int hi = P.n_seqs;
@@ -400,9 +432,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (renew) m = fmaxf(m, now);
         const float minus = m == -INFINITY ? 0.0f : -m;
         const uint64_t c2 = pack2(c, c), m2 = pack2(minus, minus);
+        uint32_t pairs[16];
 #pragma unroll
         for (int b = 0; b < 8; ++b) {                        // 16 keys: a step of P V
-          uint32_t pk[8];
+          uint32_t* pk = pairs + (b & 1) * 8;
           if (MASKED && most <= b * 16) {                    // nobody sees these keys
 #pragma unroll
             for (int i = 0; i < 8; ++i) pk[i] = 0;
@@ -417,7 +450,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               pk[i] = f32x2_to_bf16x2_bits(u, v);
             }
           }
-          tmem_st_32x8(ts + b * 8, pk);
+          if (b & 1) tmem_st_32x16(ts + (b - 1) * 8, pairs);
           if (b == kPrEarly - 1 || b == 7) {
             tmem_wait_st();
             tc_fence_before();
@@ -532,7 +565,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (!wait_long<true>(kv_empty(st), kv_ph ^ 1u, abort_flag, P.status, 1)) return false;
         // values to be cleaned arrive on a barrier of their own, whose every phase the cleaning warps see
         const uint32_t bar = clean ? v_raw(st) : kv_full(st);
-        if (lane == 0) {
+        if (elect_one()) {
           if (clean) mbar_arrive(kv_full(st));
           mbar_arrive_expect_tx(bar, L::kMat);
 #pragma unroll
@@ -562,7 +595,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             auto queries = [&](int i) -> bool {
               if (!wait_long<true>(q_empty(i), (q_ph >> i & 1u) ^ 1u, abort_flag, P.status, 1)) return false;
               q_ph ^= 1u << i;
-              if (lane == 0) {
+              if (elect_one()) {
                 mbar_arrive_expect_tx(q_full(i), L::kMat);
 #pragma unroll
                 for (int h = 0; h < HD / 64; ++h)

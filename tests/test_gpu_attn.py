@@ -466,3 +466,232 @@ def test_a_prompt_in_chunks_and_single_tokens_agree(hd, page, inter):
         have = ends
     for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
         assert np.array_equal(host(got), want)
+
+
+# ------------------------------------------------------------------------------------------------ as a program holds them
+def test_the_attention_block_from_projection_to_projection():
+    """fpt_decoder_attn_qkv, then the attention of a prompt, then a decode step of the same sequences, fpt_decoder_attn_out behind each: the
+    calls chained on one stream and one workspace give what each gives with a wait in between."""
+    from paper_2506_04985_b200 import synth
+    d, n_q, n_kv, hd, page, lens = 512, 8, 2, 64, 32, [37, 5]
+    n_qkv = (n_q + 2 * n_kv) * hd
+    wq, sq, _ = B.fpt_quantize_weights(synth.weights(n_qkv, d, 0.05, 1, "block/qkv").to(DEV))
+    wo, so, _ = B.fpt_quantize_weights(synth.weights(d, n_q * hd, 0.05, 1, "block/o").to(DEV))
+    qp_in, qp_ap = B.QParams(4, True, 0.4, 0), B.QParams(4, True, 0.1, 0)
+    total = sum(lens)
+    x = synth.activations(total, d, 1, "block/x", law="normal").to(DEV)
+    x1 = synth.activations(2, d, 2, "block/x1", law="normal").to(DEV)
+    tab = torch.from_numpy(table(64, hd)).to(DEV)
+    room = max(B.fpt_workspace_bytes(B.OP_ATTN, 1, 1, 1), B.fpt_workspace_bytes(B.OP_LINEAR, total, n_qkv, d),
+               B.fpt_workspace_bytes(B.OP_LINEAR, 2, n_qkv, d))
+
+    def run(wait):
+        stop = torch.cuda.synchronize if wait else (lambda: None)
+        ws = guarded_empty((room,), torch.uint8)
+        B.lib().fpt_reset_status(B._stream(), B._ptr(ws))
+        rng = np.random.default_rng(77)
+        cache, *_ = paged(rng, [n + 1 for n in lens], page, n_kv, hd, filled=False)
+        cu, ctx0, ctx1, ends = i32([0, 37, 42]), i32([0, 0]), i32(lens), i32([n + 1 for n in lens])
+        outs = []
+        qkv, s_n, r = B.fpt_decoder_attn_qkv(x, wq, sq, qp_in, ws=ws); stop()
+        q, k = B.fpt_rope_append(qkv, n_q, cache, tab, ctx0, cu_new=cu, want_k=True, ws=ws); stop()
+        o, _ = B.fpt_attn_prompt(q, k, qkv[:, (n_q + n_kv) * hd:], n_q, n_kv, cu, ws=ws); stop()
+        outs += [o, B.fpt_decoder_attn_out(o, wo, so, qp_ap, s_n, X=x, r=r, ws=ws)]; stop()
+        qkv, s_n, r = B.fpt_decoder_attn_qkv(x1, wq, sq, qp_in, ws=ws); stop()
+        q, _ = B.fpt_rope_append(qkv, n_q, cache, tab, ctx1, ws=ws); stop()
+        o, _ = B.fpt_attn_decode(q, cache, ends, ws=ws); stop()
+        outs += [o, B.fpt_decoder_attn_out(o, wo, so, qp_ap, s_n, X=x1, r=r, ws=ws)]
+        assert B.fpt_check_status(ws) == B.OK
+        return [t.clone() for t in outs]
+
+    a, b = run(True), run(False)
+    for u, v in zip(a, b):
+        assert torch.equal(u.view(torch.int16), v.view(torch.int16)) and torch.isfinite(u.float()).all()
+
+
+def test_decode_step_in_a_graph_follows_the_lengths_on_the_device():
+    """One captured step replayed while contexts grow: positions, lengths and pages are read from the device each time; so with
+    launches that wait for one another in the stream, and without."""
+    rng = np.random.default_rng(41)
+    hd, page, n_q, n_kv, steps, start = 128, 16, 8, 2, 20, [0, 14, 63]
+    total = [s + steps for s in start]
+    x = bf16(rng, steps, 3, (n_q + 2 * n_kv) * hd)
+    tab = table(max(total), hd)
+    tabd, ws = torch.from_numpy(tab).to(DEV), workspace()
+    for early in (True, False):
+        rng = np.random.default_rng(42)
+        cache, pages, codes, scales = paged(rng, total, page, n_kv, hd)
+        was = B.fpt_set_programmatic_launch(early)
+        try:
+            row, ctx, ends = x[0].to(DEV), i32(start), i32([s + 1 for s in start])
+            Q, O = (guarded_empty((3, n_q * hd), torch.bfloat16) for _ in range(2))
+
+            def step():
+                B.fpt_rope_append(row, n_q, cache, tabd, ctx, Q=Q, ws=ws)
+                B.fpt_attn_decode(Q, cache, ends, O=O, ws=ws)
+
+            keep = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                step()                                       # (kernels are loaded outside the capture)
+                torch.cuda.synchronize()
+                for t, old in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), keep):
+                    t.copy_(old)
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=stream):
+                    step()
+                for t in range(steps):
+                    row.copy_(x[t]), ctx.copy_(i32([s + t for s in start])), ends.copy_(i32([s + t + 1 for s in start]))
+                    g.replay()
+                    stream.synchronize()
+                    for i in range(3):
+                        y = x[t, i].float().numpy().reshape(1, -1, hd)
+                        qk = OA.rope(y[:, :n_q + n_kv], tab[start[i] + t:start[i] + t + 1], hd, False)
+                        OA.append(qk[:, n_q:], codes[0], scales[0], pages[i], start[i] + t, page)
+                        OA.append(y[:, n_q + n_kv:], codes[1], scales[1], pages[i], start[i] + t, page)
+                    if t % 7 == 0 or t == steps - 1:
+                        q = Q.float().cpu().to(torch.bfloat16)
+                        check_decode(O, None, [s + t + 1 for s in start], pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+                assert B.fpt_check_status(ws) == B.OK
+            for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+                assert np.array_equal(host(got), want)
+        finally:
+            B.fpt_set_programmatic_launch(was)
+
+
+def test_two_streams_with_a_workspace_each():
+    rng = np.random.default_rng(43)
+    hd, page, n_q, n_kv, lens = 128, 64, 8, 2, [3000, 1500]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    qd, ld = q.to(DEV), i32(lens)
+    want, _ = B.fpt_attn_decode(qd, cache, ld)
+    torch.cuda.synchronize()
+    streams, wss, outs = [torch.cuda.Stream() for _ in range(2)], [workspace() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for k in range(40):
+        with torch.cuda.stream(streams[k % 2]):
+            outs.append(B.fpt_attn_decode(qd, cache, ld, ws=wss[k % 2])[0])
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o.view(torch.int16), want.view(torch.int16))
+
+
+def test_prompt_gives_the_same_bits_each_time():
+    """Tasks go to whichever CTA is free; what a task computes does not depend on it."""
+    rng = np.random.default_rng(44)
+    hd, n_q, n_kv, lens = 128, 8, 2, [int(n) for n in rng.integers(1, 400, 40)]
+    q, k, v = (t.to(DEV) for t in prompt_case(rng, hd, n_q, n_kv, lens, lens, pad=0))
+    cu = i32(offsets(lens).tolist())
+    first, _ = B.fpt_attn_prompt(q, k, v, n_q, n_kv, cu)
+    for _ in range(5):
+        o, _ = B.fpt_attn_prompt(q, k, v, n_q, n_kv, cu)
+        assert torch.equal(o.view(torch.int16), first.view(torch.int16))
+
+
+@pytest.mark.parametrize("n", [32, 33, 128, 129, 300])
+def test_prompt_many_sequences(n):
+    """As many as a warp's lanes, as are held in registers, and more: each way of finding a task; empty ones among them."""
+    rng = np.random.default_rng(n)
+    hd, n_q, n_kv = 64, 4, 2
+    lens = [int(x) for x in rng.integers(0, 90, n)]
+    pre = [int(x) for x in rng.integers(0, 60, n)]
+    len_k = [a + b if i % 3 else a for i, (a, b) in enumerate(zip(lens, pre))]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, lens, len_k)
+    ws = workspace()
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32(offsets(len_k).tolist()),
+                               want_lse=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_prompt(o, lse, q, k, v, n_q, n_kv, hd, lens, len_k, True)
+
+
+def test_append_and_gather_many_sequences():
+    rng = np.random.default_rng(45)
+    hd, page, n_q, n_kv, n = 64, 16, 2, 1, 400
+    new, ctx = [int(x) for x in rng.integers(0, 40, n)], [int(x) for x in rng.integers(0, 40, n)]
+    cache, pages, codes, scales = paged(rng, [a + b for a, b in zip(new, ctx)], page, n_kv, hd)
+    x, tab, ws = bf16(rng, sum(new), (n_q + 2 * n_kv) * hd), table(80, hd), workspace()
+    cu = offsets(new)
+    B.fpt_rope_append(x.to(DEV), n_q, cache, torch.from_numpy(tab).to(DEV), i32(ctx), cu_new=i32(cu.tolist()), ws=ws)
+    ends = [a + b for a, b in zip(new, ctx)]
+    K, V = B.fpt_kv_gather(cache, i32(offsets(ends).tolist()), sum(ends), ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    y = x.float().numpy().reshape(-1, n_q + 2 * n_kv, hd)
+    for i in range(n):
+        if new[i]:
+            part = y[cu[i]:cu[i + 1]]
+            k = OA.rope(part[:, n_q:n_q + n_kv], tab[ctx[i]:ends[i]], hd, False)
+            OA.append(k, codes[0], scales[0], pages[i], ctx[i], page)
+            OA.append(part[:, n_q + n_kv:], codes[1], scales[1], pages[i], ctx[i], page)
+    for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+        assert np.array_equal(host(got), want)
+    for got, j in ((K, 0), (V, 1)):
+        want = np.concatenate([OA.read(codes[j], scales[j], pages[i], 0, e, page) for i, e in enumerate(ends)])
+        assert np.array_equal(bf16_host(got), torch.from_numpy(want).to(torch.bfloat16).float().numpy().reshape(got.shape))
+
+
+def test_cache_offsets_beyond_32_bits():
+    """A sequence in the last pages of a cache whose codes take more than 4 GiB."""
+    hd, page, n_q, n_kv, n_pages, n = 128, 64, 8, 8, 70_000, 200
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 10 GB")
+    k, v = (torch.zeros((n_pages, n_kv, page, hd), dtype=torch.int8, device=DEV) for _ in range(2))
+    ks, vs = (torch.zeros((n_pages, n_kv), device=DEV) for _ in range(2))
+    pages = np.array([[n_pages - 1, n_pages - 3, 1, n_pages - 2]], np.int32)
+    cache = B.KVCache(k, v, ks, vs, i32(pages.tolist()))
+    rng = np.random.default_rng(46)
+    x, tab, ws = bf16(rng, n, (n_q + 2 * n_kv) * hd), table(n, hd), workspace()
+    Q, _ = B.fpt_rope_append(x.to(DEV), n_q, cache, torch.from_numpy(tab).to(DEV), i32([0]), cu_new=i32([0, n]), ws=ws)
+    y = x.float().numpy().reshape(n, -1, hd)
+    qk = OA.rope(y[:, :n_q + n_kv], tab, hd, False)
+    local = np.array([[3, 1, 0, 2]], np.int32)                # the four pages on the host
+    codes, scales = [np.zeros((4, n_kv, page, hd), np.int8) for _ in "kv"], [np.zeros((4, n_kv), np.float32) for _ in "kv"]
+    OA.append(qk[:, n_q:], codes[0], scales[0], local[0], 0, page)
+    OA.append(y[:, n_q + n_kv:], codes[1], scales[1], local[0], 0, page)
+    for j, p in zip(local[0], pages[0]):
+        assert np.array_equal(host(k[p]), codes[0][j]) and np.array_equal(host(v[p]), codes[1][j])
+        assert np.array_equal(host(ks[p]), scales[0][j]) and np.array_equal(host(vs[p]), scales[1][j])
+    K, V = B.fpt_kv_gather(cache, i32([0, n]), n, ws=ws)
+    for got, j in ((K, 0), (V, 1)):
+        want = OA.read(codes[j], scales[j], local[0], 0, n, page).reshape(n, -1)
+        assert np.array_equal(bf16_host(got), torch.from_numpy(want).to(torch.bfloat16).float().numpy())
+    last = Q[n - 1:n]
+    o, lse = B.fpt_attn_decode(last, cache, i32([n]), want_lse=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_decode(o, lse, [n], local, codes, scales, last.cpu(), n_q, hd, page, hd ** -0.5)
+
+
+def test_append_positions_and_pages_out_of_range_are_recorded():
+    rng = np.random.default_rng(47)
+    hd, page, n_q, n_kv = 64, 16, 2, 1
+    tab = torch.from_numpy(table(50, hd)).to(DEV)
+    x = bf16(rng, 6, (n_q + 2 * n_kv) * hd).to(DEV)
+    for ctx, cu, spoil in (([45, 3], [0, 6, 6], None), ([-1, 3], [0, 3, 6], None), ([20, 3], [0, 3, 7], None), ([20, 3], [0, 4, 3], None),
+                           ([20, 3], [0, 3, 6], -1), ([20, 3], [0, 3, 6], 1 << 20)):
+        cache, pages, codes, scales = paged(rng, [30, 30], page, n_kv, hd)
+        if spoil is not None:
+            cache.pages[0, 1] = spoil
+        ws = workspace()
+        B.fpt_rope_append(x, n_q, cache, tab, i32(ctx), cu_new=i32(cu), ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX, (ctx, cu, spoil)
+        if spoil is not None:
+            assert np.array_equal(host(cache.k)[pages[0]], codes[0][pages[0]])            # nothing went to another page
+    cache, *_ = paged(rng, [30, 30], page, n_kv, hd)
+    for first, cu in (([20, 20], [0, 13, 20]), ([-1, 0], [0, 5, 10]), ([0, 0], [0, 5, 999])):
+        ws = workspace()
+        B.fpt_kv_gather(cache, i32(cu), 20, first=i32(first), ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX, (first, cu)
+
+
+def test_calls_refuse_tensors_of_the_wrong_kind():
+    rng = np.random.default_rng(48)
+    cache, *_ = paged(rng, [20], 16, 2, 64)
+    q, lens = bf16(rng, 1, 4 * 64).to(DEV), i32([20])
+    for bad in (lambda: B.fpt_attn_decode(q.float(), cache, lens), lambda: B.fpt_attn_decode(q, cache, lens.long()),
+                lambda: B.fpt_attn_decode(q, cache, lens.cpu()), lambda: B.fpt_attn_decode(q.cpu(), cache, lens),
+                lambda: B.fpt_attn_decode(q, cache, i32([20, 20])), lambda: B.fpt_attn_decode(q[:, ::2], cache, lens),
+                lambda: B.fpt_attn_decode(q, cache, lens, ws=torch.zeros(100, dtype=torch.uint8, device=DEV)),
+                lambda: B.fpt_attn_decode(q.repeat(2, 1), cache, i32([20, 20])),          # a row more than the page table has
+                lambda: B.fpt_attn_prompt(q, q[:, :128], q[:, :64], 4, 2, i32([0, 1])),
+                lambda: B.fpt_kv_gather(cache, i32([0, 20]), 20, first=lens.long())):
+        with pytest.raises(B.FptError):
+            bad()
