@@ -14,7 +14,9 @@
 //   warps 14, 15       values of the tiles that a mask cuts: those that are not finite become zeros before the tensor core
 //                      reads them (a weight of zero would not make them harmless), as do rows behind the sequence
 // While the softmax of one tile runs, the tensor core works for the other.  P (bf16) takes the place of S in tensor
-// memory; the next S of a tile is issued behind the P V that reads it, and the tensor core keeps that order.
+// memory; the next S in that place is issued behind the P V that reads it, and the tensor core keeps that order.  With heads of 64
+// there is room for a place more (kAhead): the S of a tile's next keys is there before its softmax has done with these
+// (four chunks behind prefixes, 24 heads of 64: 103 -> 95 us).
 //
 // Softmax in the exponent of two: p = 2^(S scale log2(e) - m).  m is the row's maximum when it was last renewed: it is renewed, and O in
 // tensor memory multiplied by 2^(m_old - m_new), only where the maximum has grown by more than 8, so that p <= 256; the quotient by
@@ -72,11 +74,12 @@ struct PromptParams {
 template <int HD>
 struct PrSmem {
   static constexpr int kStages = HD == 128 ? 5 : 8;
+  static constexpr int kAhead = HD == 128 ? 0 : 1;           // places of scores in tensor memory beyond one a tile
   static constexpr int kMat = kPrTile * HD * 2;              // a tile of keys, values or queries
   static constexpr int kHalf = kPrTile * 128;                // 64 of its columns: 128-byte rows
   static constexpr int kKvOff = 2 * kMat;
   static constexpr int kBarOff = kKvOff + kStages * kMat;
-  static constexpr int kNumBars = 4 + 4 * kStages + 2 + 4 + 4 + 5 + 4;
+  static constexpr int kNumBars = 4 + 4 * kStages + 2 * 13 + 1;
   static constexpr int kMiscOff = (kBarOff + kNumBars * 8 + 15) / 16 * 16;
   static constexpr int kInfoOff = kMiscOff + 32;             // (16 bytes of misc, the answer of the launch control)
   static constexpr int kStatOff = kInfoOff + 2 * 48;         // [query tile][row] {maximum, sum of weights}
@@ -309,15 +312,17 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto v_raw = [&](int s) { return bar0 + 8u * (4 + 2 * ST + s); };
   auto v_clean = [&](int s) { return bar0 + 8u * (4 + 3 * ST + s); };
   const uint32_t bar1 = bar0 + 8u * (4 + 4 * ST);
-  auto s_full = [&](int w) { return bar1 + 8u * w; };
-  auto p_full = [&](int w, int part) { return bar1 + 8u * (2 + 2 * w + part); };   // part: the first kPrEarly steps, the others
-  auto o_full = [&](int w) { return bar1 + 8u * (6 + w); };                        // a task's last P V
-  auto o_empty = [&](int w) { return bar1 + 8u * (8 + w); };
-  auto info_full = [&](int i) { return bar1 + 8u * (10 + i); };
-  auto info_empty = [&](int i) { return bar1 + 8u * (12 + i); };
-  auto stat_full = [&](int w) { return bar1 + 8u * (14 + w); };
-  auto stat_empty = [&](int w) { return bar1 + 8u * (16 + w); };
-  const uint32_t answered = bar1 + 8u * 18;
+  // With a place more, a tile's scores are issued at most one step ahead of its P V: two barriers taken in turn keep the steps apart.
+  auto s_full = [&](int w, int turn) { return bar1 + 8u * (2 * w + turn); };
+  auto p_full = [&](int w, int turn, int part) { return bar1 + 8u * (4 + 4 * w + 2 * turn + part); };   // part: the first kPrEarly steps, the others
+  auto pv_done = [&](int w) { return bar1 + 8u * (12 + w); };                      // each P V (where a place more lets S run ahead)
+  auto o_full = [&](int w) { return bar1 + 8u * (14 + w); };                       // a task's last P V
+  auto o_empty = [&](int w) { return bar1 + 8u * (16 + w); };
+  auto info_full = [&](int i) { return bar1 + 8u * (18 + i); };
+  auto info_empty = [&](int i) { return bar1 + 8u * (20 + i); };
+  auto stat_full = [&](int w) { return bar1 + 8u * (22 + w); };
+  auto stat_empty = [&](int w) { return bar1 + 8u * (24 + w); };
+  const uint32_t answered = bar1 + 8u * 26;
   float2* stats = reinterpret_cast<float2*>(smem + L::kStatOff);
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + L::kMiscOff);
   volatile uint32_t* abort_flag = misc + 1;
@@ -334,9 +339,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full(i), 1);
       mbar_init(q_empty(i), 1);
-      mbar_init(s_full(i), 1);
-      mbar_init(p_full(i, 0), 4);
-      mbar_init(p_full(i, 1), 4);
+      mbar_init(s_full(i, 0), 1);
+      mbar_init(s_full(i, 1), 1);
+      mbar_init(pv_done(i), 1);
+      for (int b = 0; b < 4; ++b) mbar_init(p_full(i, b >> 1, b & 1), 4);
       mbar_init(o_full(i), 1);
       mbar_init(o_empty(i), 4);
       mbar_init(info_full(i), 1);
@@ -360,8 +366,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
-  auto s_col = [&](int i) { return tmem + 128u * i; };
-  auto o_col = [&](int i) { return tmem + 256u + 128u * i; };
+  // A task's steps u = j nw + i (keys j, query tile i of nw) take the nw + kAhead places of scores in turn.
+  auto s_col = [&](int place) { return tmem + 128u * place; };
+  auto o_col = [&](int i) { return tmem + 128u * (2 + L::kAhead) + (uint32_t)HD * i; };
+  // Of the steps of one tile in all tasks, n before this one: which barrier, and its parity.
+  auto turn_of = [](uint32_t n) { return L::kAhead ? (int)(n & 1u) : 0; };
+  auto parity_of = [](uint32_t n) { return L::kAhead ? n >> 1 & 1u : n & 1u; };
   // (parities of barriers that come in twos are kept as bits of one word: an array indexed at run time is local memory)
   const int per_tile = kPrTile >> P.pack_log2;               // tokens
 
@@ -370,9 +380,9 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     reg_inc<kPrSoftRegs>();
     const int w = warp >> 2, r = threadIdx.x & 127;          // query tile, row of it
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = s_col(w) + lanes, to = o_col(w) + lanes;
+    const uint32_t to = o_col(w) + lanes;
     const float c = P.scale_log2;
-    uint32_t s_ph = 0, stat_ph = 0;
+    uint32_t step = 0, stat_ph = 0;                           // step: of this tile in all tasks
     bool ok = true;
     for (int n = 0; ok; ++n) {
       if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 7)) break;
@@ -385,14 +395,16 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       if (lane == 0) mbar_arrive(info_empty(n & 1));
       if (!(flags & 1)) break;
       if (w == 1 && !(flags & 2)) continue;
+      int place = w;
       float m = -INFINITY;                                   // of S * c, when last renewed
       uint64_t sum2[2] = {0, 0};                             // four partial sums of weights
       // One tile of keys; MASKED: some row of the task does not see all of it.
       auto tile = [&](int j, auto masked) -> bool {
         constexpr bool MASKED = decltype(masked)::value;
-        if (!wait_long<true>(s_full(w), s_ph, abort_flag, P.status, 4)) return false;
-        s_ph ^= 1u;
+        if (!wait_long<true>(s_full(w, turn_of(step)), parity_of(step), abort_flag, P.status, 4)) return false;
         tc_fence_after();
+        const uint32_t ts = s_col(place) + lanes;
+        if (L::kAhead) place = place > 0 ? place - 1 : (flags & 2) ? 2 : 1;    // nw further, modulo nw + 1
         float x[128];
 #pragma unroll
         for (int b = 0; b < 4; ++b) tmem_ld_32x32(ts + b * 32, reinterpret_cast<uint32_t(&)[32]>(x[b * 32]));
@@ -415,7 +427,12 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;     // c > 0; a NaN stays in its weight
         const bool renew = now > m + 8.0f || m == -INFINITY;
         if (j > 0 && __any_sync(0xffffffffu, renew && now > m)) {
-          // (the P V before is done: the S just read was issued behind it)
+          // The P V before has to be done.  Without a place more it is: the S just read was issued behind it.  With one, that holds of
+          // the P V before that: the barrier is at most one phase behind, and its parity says whether it is.
+          if (L::kAhead) {
+            if (!wait_long<true>(pv_done(w), (step + 1u) & 1u, abort_flag, P.status, 4)) return false;
+            tc_fence_after();
+          }
           const float f = renew && now > m ? (m == -INFINITY ? 0.0f : pow2_unit(m - now)) : 1.0f;
           sum2[0] = mul2(sum2[0], pack2(f, f));
           sum2[1] = mul2(sum2[1], pack2(f, f));
@@ -455,9 +472,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_full(w, b == 7));
+            if (lane == 0) mbar_arrive(p_full(w, turn_of(step), b == 7));
           }
         }
+        ++step;
         return true;
       };
       for (int j = 0; ok && j < plain; ++j) ok = tile(j, std::false_type{});
@@ -636,26 +654,18 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       // ---------------------------------------------------------------- tensor core
       if (elect_one()) {
         constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128, false), idesc_o = umma_idesc_bf16(128, HD, true);
-        int st = 0; uint32_t ph = 0;                          // ring: keys 0, values 0, keys 1, ... of all tasks
-        int k_st = 0, v_st = 0;
+        int k_at = 0, v_at = 1; uint32_t k_ph = 0, v_ph = 0;  // ring: keys 0, values 0, keys 1, ... of all tasks
         uint32_t clean_par = 0;                               // per stage: parity of the next phase of v_clean
-        uint32_t q_ph = 0, o_ph = 0, p_ph = 0;
+        uint32_t q_ph = 0, o_ph = 0;
+        uint32_t done = 0;                                    // two bits a tile: its steps in the tasks before, modulo 4
         bool ok = true;
-        auto next = [&](int& mine) {
-          mine = st;
+        // the next keys or the next values: their stage, once it is filled
+        auto next = [&](int& at, uint32_t& ph, int& st) -> bool {
+          st = at;
           const bool got = wait_long<false>(kv_full(st), ph, abort_flag, P.status, 2);
-          if (++st == ST) { st = 0; ph ^= 1u; }
+          at += 2;
+          if (at >= ST) { at -= ST; ph ^= 1u; }
           return got;
-        };
-        auto scores = [&](int i) {
-          const uint32_t a = sbase + i * L::kMat, b = sbase + L::kKvOff + k_st * L::kMat;
-#pragma unroll
-          for (int h = 0; h < HD / 64; ++h) {
-            const uint64_t ad = umma_desc_kmajor_sw128(a + h * L::kHalf), bd = umma_desc_kmajor_sw128(b + h * L::kHalf);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(s_col(i), ad + 2u * k, bd + 2u * k, idesc_s, (h | k) != 0);
-          }
-          umma_commit(s_full(i));
         };
         for (int n = 0; ok; ++n) {
           if (!wait_long<false>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 2)) break;
@@ -665,18 +675,32 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           if (!(flags & 1)) break;
           if (tiles == 0) continue;
           const int nw = (flags & 2) ? 2 : 1;
-          ok = next(k_st);
-          for (int i = 0; ok && i < nw; ++i) {
-            ok = wait_long<false>(q_full(i), q_ph >> i & 1u, abort_flag, P.status, 2);
-            q_ph ^= 1u << i;
-            if (!ok) break;
+          int k_st = 0, v_st = 0, s_place = 0, p_place = 0;
+          auto after = [&](int place) { return place + 1 == nw + L::kAhead ? 0 : place + 1; };
+          auto scores = [&](int j, int i) -> bool {
+            if (i == 0 && !next(k_at, k_ph, k_st)) return false;
+            if (j == 0) {
+              if (!wait_long<false>(q_full(i), q_ph >> i & 1u, abort_flag, P.status, 2)) return false;
+              q_ph ^= 1u << i;
+            }
             tc_fence_after();
-            scores(i);
-            if (tiles == 1) umma_commit(q_empty(i));
-          }
-          if (ok) umma_commit(kv_empty(k_st));
+            const uint32_t a = sbase + i * L::kMat, b = sbase + L::kKvOff + k_st * L::kMat, d = s_col(L::kAhead ? s_place : i);
+#pragma unroll
+            for (int h = 0; h < HD / 64; ++h) {
+              const uint64_t ad = umma_desc_kmajor_sw128(a + h * L::kHalf), bd = umma_desc_kmajor_sw128(b + h * L::kHalf);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) umma_bf16(d, ad + 2u * k, bd + 2u * k, idesc_s, (h | k) != 0);
+            }
+            umma_commit(s_full(i, turn_of((done >> 2 * i) + (uint32_t)j)));
+            if (j + 1 == tiles) umma_commit(q_empty(i));
+            if (i == nw - 1) umma_commit(kv_empty(k_st));
+            s_place = after(s_place);
+            return true;
+          };
+          for (int i = 0; ok && i < nw; ++i) ok = scores(0, i);
+          if (L::kAhead && ok && tiles > 1) ok = scores(1, 0);
           for (int j = 0; ok && j < tiles; ++j) {
-            ok = next(v_st);
+            ok = next(v_at, v_ph, v_st);
             if (ok && j >= cut) {
               ok = wait_long<false>(v_clean(v_st), (clean_par >> v_st) & 1u, abort_flag, P.status, 3);
               clean_par ^= 1u << v_st;
@@ -687,25 +711,25 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 o_ph ^= 1u << i;
               }
               const uint64_t bd = umma_desc_mnmajor_sw128(sbase + L::kKvOff + v_st * L::kMat, L::kHalf);
+              const uint32_t step = (done >> 2 * i) + (uint32_t)j, p = s_col(L::kAhead ? p_place : i);
               for (int part = 0; ok && part < 2; ++part) {
-                ok = wait_long<false>(p_full(i, part), p_ph >> i & 1u, abort_flag, P.status, 3);
+                ok = wait_long<false>(p_full(i, turn_of(step), part), parity_of(step), abort_flag, P.status, 3);
                 if (!ok) break;
                 tc_fence_after();
                 for (int k = part ? kPrEarly : 0; k < (part ? kPrTile / 16 : kPrEarly); ++k)
-                  umma_bf16_ts(o_col(i), s_col(i) + 8u * k, bd + 128u * k, idesc_o, (j | k) != 0);
+                  umma_bf16_ts(o_col(i), p + 8u * k, bd + 128u * k, idesc_o, (j | k) != 0);
               }
               if (!ok) break;
-              p_ph ^= 1u << i;
+              if (L::kAhead) umma_commit(pv_done(i));
               if (j + 1 == tiles) umma_commit(o_full(i));
               if (i == nw - 1) umma_commit(kv_empty(v_st));
-              if (j + 1 < tiles) {
-                if (i == 0 && !(ok = next(k_st))) break;
-                scores(i);
-                if (j + 2 == tiles) umma_commit(q_empty(i));
-                if (i == nw - 1) umma_commit(kv_empty(k_st));
-              }
+              p_place = after(p_place);
+              // the scores that take this place: nw + kAhead steps on
+              const int to_i = L::kAhead ? (nw == 2 ? 1 - i : 0) : i, to_j = L::kAhead ? (nw == 2 ? j + 1 + i : j + 2) : j + 1;
+              if (to_j < tiles) ok = scores(to_j, to_i);
             }
           }
+          done = ((done & 3u) + (uint32_t)tiles & 3u) | (nw == 2 ? ((done >> 2) + (uint32_t)tiles & 3u) << 2 : done & 12u);
         }
       }
     } else {
