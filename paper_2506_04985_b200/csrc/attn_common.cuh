@@ -96,7 +96,11 @@ constexpr int kAttnMaxCtas = 640;         // launches of the single-token attent
 // A part of a row's result in the workspace: for at most 16 query heads the sums [head_dim], the reference exponent and the
 // sum of weights, float32.
 constexpr int kAttnPartFloats = 16 * (128 + 2);
-constexpr size_t kAttnScratchBytes = (size_t)kAttnMaxCtas * 2 * kAttnPartFloats * 4;
+// The attention of prompts keeps the sums of at most this many parts of 256 rows of 128 (of 64: twice as many), maxima, sums of weights and
+// a flag beside them.
+constexpr int kAttnPromptParts = 125;
+constexpr size_t kAttnScratchBytes = (size_t)kAttnPromptParts * 256 * (128 + 3) * 4;
+static_assert(kAttnScratchBytes >= (size_t)kAttnMaxCtas * 2 * kAttnPartFloats * 4, "the single-token attention's parts");
 inline size_t attn_workspace_bytes() { return kStatusBytes + kAttnScratchBytes; }
 
 }  // namespace fpt

@@ -695,3 +695,83 @@ def test_calls_refuse_tensors_of_the_wrong_kind():
                 lambda: B.fpt_kv_gather(cache, i32([0, 20]), 20, first=lens.long())):
         with pytest.raises(B.FptError):
             bad()
+
+
+# ------------------------------------------------------------------------------------------------ few query rows, many keys
+SPLIT = [
+    # hd, n_q, n_kv, len_q, len_k (None: the same), causal
+    (128, 32, 8, [64], [3000], True),
+    (128, 4, 1, [1], [5000], True),
+    (64, 24, 4, [100], [2777], True),
+    (64, 8, 1, [33, 0, 70, 5], [1500, 900, 4000, 5], True),
+    (128, 8, 2, [300], [2000], False),
+    (128, 7, 1, [129, 3], [4000, 640], True),
+    (64, 2, 2, [1700], None, True),                          # tasks of fewer tiles than the longest has parts
+    (128, 2, 1, [600, 2], [100, 3333], True),                # rows that see nothing beside a long walk
+    (128, 16, 1, [5] * 32, [2000 + 13 * i for i in range(32)], True),
+    (64, 1, 1, [3], [20000], True),
+]
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,len_q,len_k,causal", SPLIT)
+def test_prompt_keys_in_parts(hd, n_q, n_kv, len_q, len_k, causal):
+    same, len_k = len_k is None, len_k or len_q
+    rng = np.random.default_rng(sum(len_q) + hd + n_q + 1)
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, len_q, len_k)
+    k[sum(len_k):] = math.nan
+    v[sum(len_k):] = math.inf
+    out = guarded_empty(q.shape, torch.bfloat16)
+    out.fill_(7.0)
+    room = B.fpt_workspace_bytes(B.OP_ATTN, 1, 1, 1)
+    ws = torch.full((room + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    B.lib().fpt_reset_status(B._stream(), B._ptr(ws))
+    _, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32(offsets(len_q).tolist()),
+                               cu_k=None if same else i32(offsets(len_k).tolist()), causal=causal, want_lse=True, O=out, ws=ws[:room])
+    assert B.fpt_check_status(ws) == B.OK
+    assert (ws[room:] == 0x5A).all()
+    check_prompt(out, lse, q, k, v, n_q, n_kv, hd, len_q, len_k, causal)
+    assert (bf16_host(out)[sum(len_q):] == 7).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_parts_and_odd_values(hd):
+    """Infinities and NaN in several parts' keys and values reach the queries that see them and no others."""
+    rng = np.random.default_rng(51)
+    n_q, n_kv, len_q, len_k = 4, 2, [100], [3000]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, len_q, len_k, pad=0)
+    v[2950, 3] = math.inf
+    v[2990, 5] = math.nan
+    v[1000, hd + 2] = math.nan                           # the second head, seen by every query
+    k[2980, :hd] = math.nan
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32([0, 100]), cu_k=i32([0, 3000]), want_lse=True)
+    args = [t.float().numpy().reshape(t.shape[0], -1, hd) for t in (q, k, v)]
+    want, _, spread, mass = OA.attend(*args, hd ** -0.5, True)
+    got = bf16_host(o).reshape(want.shape)
+    fine = np.isfinite(want)
+    assert fine.any() and not fine.all()
+    assert (np.isfinite(got) == fine).all()
+    assert (np.abs(got - want)[fine] <= out_bound(want, spread, mass, hd, HALF)[fine]).all()
+
+
+def test_prompt_parts_captured_replayed_and_the_same_bits():
+    """The sums of parts lie in the workspace: replays between other calls with it give the same bits."""
+    rng = np.random.default_rng(52)
+    hd, n_q, n_kv = 128, 8, 2
+    q, k, v = (t.to(DEV) for t in prompt_case(rng, hd, n_q, n_kv, [90], [4000], pad=0))
+    a, b, ws = i32([0, 90]), i32([0, 4000]), workspace()
+    first, lse1 = B.fpt_attn_prompt(q, k, v, n_q, n_kv, a, cu_k=b, want_lse=True, ws=ws)
+    out = torch.empty_like(first)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _, lse = B.fpt_attn_prompt(q, k, v, n_q, n_kv, a, cu_k=b, want_lse=True, O=out, ws=ws)
+    page, lens = 64, [700, 9000]
+    cache, pages, codes, scales, qd = decode_case(rng, hd, page, n_q, n_kv, lens)
+    want, _ = B.fpt_attn_decode(qd.to(DEV), cache, i32(lens))
+    for _ in range(4):
+        out.fill_(0)
+        lse.fill_(0)
+        g.replay()
+        o, _ = B.fpt_attn_decode(qd.to(DEV), cache, i32(lens), ws=ws)
+        assert torch.equal(out.view(torch.int16), first.view(torch.int16)) and torch.equal(lse, lse1)
+        assert torch.equal(o.view(torch.int16), want.view(torch.int16))
+    assert B.fpt_check_status(ws) == B.OK
