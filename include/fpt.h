@@ -402,8 +402,8 @@ typedef struct fpt_kv_cache {
  *        a' = a cos - b sin,  b' = b cos + a sin
  *   Q_out [M, ld_q], n_q heads; K_out [M, ld_k], n_kv heads, or NULL.  Each may be its own place in QKV (same address
  *        and leading dimension); otherwise they overlap nothing.
- *   cache NULL or cache->k NULL: no append (n_kv and head_dim are then read from the struct all the same, so it is
- *        required).  With it, for each page and head that gets new tokens:
+ *   cache required; with cache->k NULL nothing is appended, and only its n_kv and head_dim are read.  Otherwise, for
+ *        each page and head that gets new tokens:
  *        m = max |v| over the new finite values, keys after their rounding to bf16
  *        s = max(s_old, m / 127), s_old = 0 where the page held no earlier token of the sequence  (float32 division)
  *        inv = 1 / s  (0 where s < 2^-126: such a page holds zeros)
@@ -442,8 +442,10 @@ int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, const fpt_kv
  * causal = 1 only those with j <= i + (len_k - len_q), so that the last query sees the last key; a row that sees none gives O = 0, lse = -inf.
  *   Q [M_q, ld_q], K and V [M_k, ld_k], [M_k, ld_v], O [M_q, ld_o] bf16; lse [M_q, n_q] f32 or NULL
  *   cu_q, cu_k [n_seqs + 1]; cu_k NULL: cu_q.  Q, K and V may be places in one buffer; O overlaps none of them.
- * float32 scores and sums; the weights enter the second product in bf16.  Values of hidden keys, infinities and NaN
- * among them, reach no result.
+ * float32 scores and sums; the weights enter the second product in bf16, scaled so that a row's largest is at most 2^8: values below
+ * 2^119 / len_k in magnitude overflow no sum.  Values of hidden keys, infinities and NaN among them, reach no result.
+ * Where few query rows would leave SMs idle, keys are split over them by the sizes and the lengths of all sequences, and a
+ * second launch joins the parts: the same call gives the same bits, another batch may round a sequence's sums otherwise.
  */
 int fpt_attn_prompt(void* stream, const void* Q, int ld_q, int M_q, const void* K, int ld_k, const void* V, int ld_v,
                     int M_k, int n_q, int n_kv, int head_dim, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,

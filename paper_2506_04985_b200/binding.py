@@ -3,15 +3,19 @@
 Every function has the name of the C entry point it calls and takes torch CUDA tensors
 where the C function takes device pointers.  torch is used for device memory and the
 current stream, nothing else; no step of the path runs in Python or in torch ops.
-A missing or unloadable library raises at first use: there is no fallback.
+A missing or unloadable library raises at first use: there is no fallback.  (The attention calls go
+through a small extension, csrc/calls.cpp, which marshals the same way in a third of the time.)
 """
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfpt_b200.so")
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
 
 OK = 0
 ERR_BAD_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = -1, -2, -3, -4, -5, -6, -7
@@ -47,24 +51,14 @@ class _KVCacheStruct(ctypes.Structure):
 class KVCache:
     """A paged 8-bit cache (see `fpt_kv_cache`): codes int8 [n_pages, n_kv, page, head_dim], scales f32 [n_pages, n_kv],
     page table int32 [n_seqs, max_pages], all contiguous on one device."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "dev", "struct", "ref")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "dev", "ref")
 
     def __init__(self, k, v, k_scale, v_scale, pages):
-        shape = k.shape
-        n_pages, n_kv, page, hd = shape
-        if not (k.dtype is torch.int8 and v.dtype is torch.int8 and k_scale.dtype is torch.float32 and
-                v_scale.dtype is torch.float32 and pages.dtype is torch.int32 and v.shape == shape and
-                k_scale.shape == shape[:2] and v_scale.shape == shape[:2] and pages.dim() == 2 and k.is_contiguous() and
-                v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous() and pages.is_contiguous()):
-            raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table are wanted")
+        described = (_calls or _native()).describe_cache(k, v, k_scale, v_scale, pages)
+        if described is None:
+            raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table on one device are wanted")
         self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
-        self.n_kv, self.head_dim, self.dev = n_kv, hd, k.get_device()
-        if not (self.dev == v.get_device() == k_scale.get_device() == v_scale.get_device() == pages.get_device()):
-            raise ValueError("KVCache: tensors of one device are wanted")
-        self.n_seqs, max_pages = pages.shape
-        self.struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages.data_ptr(),
-                                     n_pages, n_kv, page, hd, max_pages)
-        self.ref = ctypes.byref(self.struct)
+        self.ref, self.n_seqs, self.n_kv, self.head_dim, self.dev = described         # ref: the struct's bytes
 
     @classmethod
     def heads(cls, n_kv, head_dim):
@@ -72,8 +66,7 @@ class KVCache:
         c = cls.__new__(cls)
         c.k = c.v = c.k_scale = c.v_scale = c.pages = None
         c.n_seqs, c.n_kv, c.head_dim, c.dev = 0, n_kv, head_dim, -1
-        c.struct = _KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0)
-        c.ref = ctypes.byref(c.struct)
+        c.ref = bytes(_KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0))
         return c
 
 
@@ -84,6 +77,7 @@ class FptError(RuntimeError):
 
 
 _lib = None
+_calls = None
 _allocator = None
 
 
@@ -92,6 +86,14 @@ def set_allocator(fn):
     (None: plain torch.empty).  The GPU tests install one that surrounds each buffer with guard bands."""
     global _allocator
     _allocator = fn
+    if _calls is not None:
+        _calls.set_allocator(_for_calls(fn))
+
+
+def _for_calls(fn):
+    if fn is None:
+        return None
+    return lambda f32, rows, cols, dev: fn((rows, cols), torch.float32 if f32 else torch.bfloat16, torch.device("cuda", dev))
 
 
 def _empty(shape, dtype, device):
@@ -141,6 +143,23 @@ def lib():
                 getattr(L, name).restype = ci
         _lib = L
     return _lib
+
+
+def _native():
+    """The extension that marshals the attention calls (loads it on first use; raises if it is not there)."""
+    global _calls
+    if _calls is None:
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError(f"{CALLS_PATH} is missing: build it with `python -m paper_2506_04985_b200.build`")
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("_calls", CALLS_PATH)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_calls", CALLS_PATH, loader=loader))
+        loader.exec_module(m)
+        m.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
+                 for f in ("fpt_rope_append", "fpt_kv_gather", "fpt_attn_decode", "fpt_attn_prompt")), FptError)
+        m.set_allocator(_for_calls(_allocator))
+        _calls = m
+    return _calls
 
 
 # What every call goes through.  A small linear spends more time here than on the GPU, so addresses and the stream are
@@ -354,139 +373,43 @@ def new_kv_cache(n_pages, n_kv, page, head_dim, pages, device="cuda"):
     return KVCache(k, v, ks, vs, pages)
 
 
-# What the attention calls ask of a tensor (their rows may be places in a wider buffer), and how they allocate: a decode step's
-# kernel takes about as long as these lines, so an attribute is read once, and what resembles an input is made from it
-# (torch.empty_like and new_empty cost half of torch.empty).
-def _bad(where):
-    return FptError(ERR_BAD_ARG, where)
-
-
-def _rows(t, dev, where):
-    """Leading dimension of a bf16 [rows, columns] tensor on device `dev` whose rows are contiguous."""
-    strides = t.stride()
-    if t.dtype is not torch.bfloat16 or len(strides) != 2 or strides[1] != 1 or t.get_device() != dev:
-        raise _bad(where)
-    ld, (rows, cols) = strides[0], t.shape
-    return ld if rows > 1 or ld >= cols else cols
-
-
-def _i32(t, n, dev, where):
-    """Address of an int32 [n] tensor on device `dev`."""
-    if t.dtype is not torch.int32 or t.shape != (n,) or (n > 1 and t.stride() != (1,)) or t.get_device() != dev:
-        raise _bad(where)
-    return t.data_ptr()
-
-
-def _scratch(ws, dev, where):
-    """Address and size of a workspace on device `dev`, which has to be the current one (a new workspace for None)."""
-    if dev != (_device() if _device is not None else torch.cuda.current_device()):
-        raise _bad(where)
-    if ws is None:
-        ws = new_workspace(OP_ATTN, 1, 1, 1, torch.device("cuda", dev))
-    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
-        raise _bad(where)
-    return ws.data_ptr(), ws.numel()
-
-
-def _like(t):
-    return torch.empty_like(t) if _allocator is None else _empty(t.shape, t.dtype, t.device)
-
-
-def _new(t, shape, dtype):
-    return t.new_empty(shape, dtype=dtype) if _allocator is None else _empty(shape, dtype, t.device)
+# The attention calls: tensors are checked, and outputs made, in csrc/calls.cpp.
+def _scratch(t, where):
+    """A new workspace beside tensor `t`."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise FptError(ERR_BAD_ARG, where)
+    return new_workspace(OP_ATTN, 1, 1, 1, t.device)
 
 
 def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, want_k=False, Q=None, K=None, ws=None):
     """QKV [M, (n_q + 2 n_kv) head_dim] bf16, rope f32 [n_pos, rot_dim / 2, 2], ctx int32 [n_seqs], cu_new int32 [n_seqs + 1]
     (None: row s is sequence s's token) -> (rotated queries bf16 [M, n_q head_dim], rotated keys [M, n_kv head_dim] or None).
     Keys and values go to the cache (KVCache.heads(n_kv, head_dim): nowhere)."""
-    where = "fpt_rope_append"
-    M, cols = QKV.shape
-    hd, n_kv, n = cache.head_dim, cache.n_kv, ctx.shape[0]
-    n_pos, pairs, two = rope.shape
-    dev = QKV.get_device()
-    scratch = _scratch(ws, dev, where)
-    if (rope.dtype is not torch.float32 or two != 2 or not rope.is_contiguous() or rope.get_device() != dev or
-            cols < (n_q + 2 * n_kv) * hd or (cache.pages is not None and (cache.n_seqs < n or cache.dev != dev))):
-        raise _bad(where)
-    if Q is None:
-        Q = _new(QKV, (M, n_q * hd), torch.bfloat16)
-    elif Q.shape != (M, n_q * hd):
-        raise _bad(where)
-    if K is None:
-        if want_k:
-            K = _new(QKV, (M, n_kv * hd), torch.bfloat16)
-    elif K.shape != (M, n_kv * hd):
-        raise _bad(where)
-    _check(lib().fpt_rope_append(_stream(), QKV.data_ptr(), M, _rows(QKV, dev, where), n_q, rope.data_ptr(), n_pos, 2 * pairs, layout,
-                                 None if cu_new is None else _i32(cu_new, n + 1, dev, where), _i32(ctx, n, dev, where), n, cache.ref,
-                                 Q.data_ptr(), _rows(Q, dev, where), None if K is None else K.data_ptr(),
-                                 0 if K is None else _rows(K, dev, where), *scratch), where)
-    return Q, K
+    if ws is None:
+        ws = _scratch(QKV, "fpt_rope_append")
+    return (_calls or _native()).rope_append(QKV, n_q, cache.ref, cache.n_seqs, cache.dev, rope, ctx, cu_new, layout, want_k, Q, K, ws)
 
 
 def fpt_kv_gather(cache, cu_out, M, first=None, K=None, V=None, ws=None):
     """Cached tokens first[s] ... of every sequence in bf16 -> (K, V) [M, n_kv head_dim], packed by cu_out int32 [n_seqs + 1]."""
-    where = "fpt_kv_gather"
-    n, shape = cu_out.shape[0] - 1, (M, cache.n_kv * cache.head_dim)
-    dev = cache.dev
-    if cache.pages is None or cache.n_seqs < n:
-        raise _bad(where)
-    scratch = _scratch(ws, dev, where)
-    if K is None:
-        K = _new(cu_out, shape, torch.bfloat16)
-    if V is None:
-        V = _like(K) if K.is_contiguous() else _new(cu_out, shape, torch.bfloat16)
-    ld = _rows(K, dev, where)
-    if _rows(V, dev, where) != ld or K.shape != shape or V.shape != shape:
-        raise _bad(where)
-    _check(lib().fpt_kv_gather(_stream(), cache.ref, None if first is None else _i32(first, n, dev, where),
-                               _i32(cu_out, n + 1, dev, where), n, M, K.data_ptr(), V.data_ptr(), ld, *scratch), where)
-    return K, V
+    if ws is None:
+        ws = _scratch(cu_out, "fpt_kv_gather")
+    return (_calls or _native()).kv_gather(cache.ref, cache.n_seqs, cache.dev, cu_out, M, first, K, V, ws)
 
 
 def fpt_attn_decode(Q, cache, kv_len, scale=None, want_lse=False, O=None, ws=None):
     """Q [n_seqs, n_q head_dim] bf16, kv_len int32 [n_seqs] -> (O like Q, lse f32 [n_seqs, n_q] or None)."""
-    where = "fpt_attn_decode"
-    n, cols = shape = Q.shape
-    hd = cache.head_dim
-    n_q = cols // hd
-    dev = cache.dev
-    if cache.n_seqs < n or cols != n_q * hd:
-        raise _bad(where)
-    scratch = _scratch(ws, dev, where)
-    if O is None:
-        O = _like(Q)
-    elif O.shape != shape:
-        raise _bad(where)
-    lse = _new(Q, (n, n_q), torch.float32) if want_lse else None
-    _check(lib().fpt_attn_decode(_stream(), Q.data_ptr(), _rows(Q, dev, where), n_q, cache.ref, _i32(kv_len, n, dev, where), n,
-                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, dev, where),
-                                 None if lse is None else lse.data_ptr(), *scratch), where)
-    return O, lse
+    if ws is None:
+        ws = _scratch(Q, "fpt_attn_decode")
+    return (_calls or _native()).attn_decode(Q, cache.ref, cache.n_seqs, cache.dev, kv_len, scale, want_lse, O, ws)
 
 
 def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None, want_lse=False, O=None, ws=None):
     """Q [M_q, n_q head_dim], K and V [M_k, n_kv head_dim] bf16 (places in wider buffers will do), packed by cu_q, cu_k int32
     [n_seqs + 1] (cu_k None: cu_q) -> (O like Q, lse f32 [M_q, n_q] or None)."""
-    where = "fpt_attn_prompt"
-    Mq, cols = shape = Q.shape
-    Mk, cols_k = K.shape
-    hd, n, dev = cols // max(n_q, 1), cu_q.shape[0] - 1, Q.get_device()
-    scratch = _scratch(ws, dev, where)
-    if cols != n_q * hd or cols_k != n_kv * hd or V.shape != K.shape:
-        raise _bad(where)
-    if O is None:
-        O = _like(Q)
-    elif O.shape != shape:
-        raise _bad(where)
-    lse = _new(Q, (Mq, n_q), torch.float32) if want_lse else None
-    _check(lib().fpt_attn_prompt(_stream(), Q.data_ptr(), _rows(Q, dev, where), Mq, K.data_ptr(), _rows(K, dev, where),
-                                 V.data_ptr(), _rows(V, dev, where), Mk, n_q, n_kv, hd, _i32(cu_q, n + 1, dev, where),
-                                 None if cu_k is None else _i32(cu_k, n + 1, dev, where), n, int(bool(causal)),
-                                 hd ** -0.5 if scale is None else scale, O.data_ptr(), _rows(O, dev, where),
-                                 None if lse is None else lse.data_ptr(), *scratch), where)
-    return O, lse
+    if ws is None:
+        ws = _scratch(Q, "fpt_attn_prompt")
+    return (_calls or _native()).attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k, causal, scale, want_lse, O, ws)
 
 
 def fpt_act_quant_dynamic(X, bits=4, flags=RMSNORM, eps=1e-5, s_in=None, want_s_out=True, out=None):

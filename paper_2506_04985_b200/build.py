@@ -1,9 +1,9 @@
-"""Builds the C-ABI shared library in-tree with nvcc for sm_100a.
+"""Builds the C-ABI shared library in-tree with nvcc for sm_100a, and the extension that marshals its attention calls.
 
     python -m paper_2506_04985_b200.build [-v]
 
-The library is a plain `nvcc -shared` of csrc/*.cu (no torch headers); it is rebuilt
-when a source is newer than the binary.
+The library is a plain `nvcc -shared` of csrc/*.cu (no torch headers), the extension a `g++ -shared` of csrc/calls.cpp
+against torch's headers and libraries; each is rebuilt when a source is newer than the binary.
 """
 import glob
 import os
@@ -17,6 +17,10 @@ DEPS = SRC + sorted(glob.glob(os.path.join(HERE, "csrc", "*.cuh")) + glob.glob(o
     os.path.join(os.path.dirname(HERE), "include", "fpt.h")]
 
 
+CALLS = os.path.join(HERE, "_calls.so")
+CALLS_SRC = os.path.join(HERE, "csrc", "calls.cpp")
+
+
 def nvcc_path():
     for cand in (os.environ.get("NVCC"), "/usr/local/cuda/bin/nvcc", "nvcc"):
         if cand and (os.path.isabs(cand) and os.path.exists(cand) or not os.path.isabs(cand)):
@@ -24,25 +28,48 @@ def nvcc_path():
     return "nvcc"
 
 
-def needs_build():
-    if not os.path.exists(LIB):
+def _older(binary, sources):
+    if not os.path.exists(binary):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(f) > t for f in DEPS)
+    t = os.path.getmtime(binary)
+    return any(os.path.getmtime(f) > t for f in sources)
+
+
+def needs_build():
+    return _older(LIB, DEPS)
+
+
+def _run(cmd, what, verbose):
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if verbose or r.returncode != 0:
+        sys.stderr.write(r.stdout)
+    if r.returncode != 0:
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed building " + what)
+
+
+def build_calls(verbose=False, force=False):
+    if not force and not _older(CALLS, [CALLS_SRC, DEPS[-1]]):
+        return CALLS
+    import sysconfig
+    import torch
+    top = os.path.dirname(torch.__file__)
+    inc = [os.path.join(top, "include"), os.path.join(top, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc_path()))), "include")]
+    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared"] + [f for i in inc for f in ("-isystem", i)] +
+           [CALLS_SRC, "-o", CALLS, "-L" + os.path.join(top, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    _run(cmd, CALLS, verbose)
+    return CALLS
 
 
 def build(verbose=False, force=False):
+    build_calls(verbose, force)
     if not force and not needs_build():
         return LIB
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-Xcompiler", "-fPIC", "-shared", "-o", LIB] + SRC
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if verbose or r.returncode != 0:
-        sys.stderr.write(r.stdout)
-    if r.returncode != 0:
-        raise RuntimeError("nvcc failed building " + LIB)
+    _run(cmd, LIB, verbose)
     return LIB
 
 

@@ -10,6 +10,10 @@
     python -m paper_2506_04985_b200.microbench gemm_a8   --M 2048 --N 6144 --K 4096       (int8 activation codes)
     python -m paper_2506_04985_b200.microbench linear_dynamic --M 2048 --N 6144 --K 4096 --bits 4
     python -m paper_2506_04985_b200.microbench act_quant_dynamic --M 2048 --K 4096 --bits 4
+    python -m paper_2506_04985_b200.microbench attn_prompt --seqs 1 --M 2048 --prefix 0   (--heads 32 --kv-heads 8 --head-dim 128)
+    python -m paper_2506_04985_b200.microbench attn_decode --seqs 64 --M 4096             (M cached tokens a sequence, --page 64)
+    python -m paper_2506_04985_b200.microbench rope_append --seqs 64 --M 1 --prefix 1000  (M new tokens a sequence behind a prefix)
+    python -m paper_2506_04985_b200.microbench kv_gather   --seqs 4 --M 8192
     python -m paper_2506_04985_b200.microbench mma_probe                                  (bare tensor-core instruction rates)
 
 Operands are random packed codes / random bf16 values made on the device (timing does
@@ -136,6 +140,52 @@ def make_case(kind, M, N, K, sets, dev, f16_scales=False, bits=4):
     raise ValueError(kind)
 
 
+def make_attn_case(kind, seqs, M, prefix, n_q, n_kv, hd, page, sets, dev):
+    """The same for the attention calls: `seqs` sequences of M tokens each, behind `prefix` tokens where the call knows of such."""
+    def offsets(n):
+        return torch.arange(0, (seqs + 1) * n, n, dtype=torch.int32, device=dev)
+
+    def a_cache(tokens):
+        per = -(-tokens // page)
+        pages = torch.randperm(seqs * per, device=dev).to(torch.int32).view(seqs, per)
+        c = B.new_kv_cache(seqs * per, n_kv, page, hd, pages, dev)
+        for codes, scales in ((c.k, c.k_scale), (c.v, c.v_scale)):
+            codes.random_(-127, 128)
+            scales.uniform_(0.01, 0.02)
+        return c
+
+    runs = []
+    ctx, rows, kv = prefix + M, seqs * M, n_kv * hd
+    for _ in range(sets):
+        ws = B.new_workspace(B.OP_ATTN, 1, 1, 1, dev)
+        if kind == "attn_prompt":
+            q, k, v = _bf16(rows, n_q * hd, dev), _bf16(seqs * ctx, kv, dev), _bf16(seqs * ctx, kv, dev)
+            cu_q, cu_k, o = offsets(M), offsets(ctx), torch.empty_like(q)
+            runs.append(lambda q=q, k=k, v=v, cu_q=cu_q, cu_k=cu_k, o=o, ws=ws: B.fpt_attn_prompt(q, k, v, n_q, n_kv, cu_q, cu_k=cu_k, O=o, ws=ws))
+        elif kind == "attn_decode":
+            q, c = _bf16(seqs, n_q * hd, dev), a_cache(M)
+            n, o = torch.full((seqs,), M, dtype=torch.int32, device=dev), torch.empty_like(q)
+            runs.append(lambda q=q, c=c, n=n, o=o, ws=ws: B.fpt_attn_decode(q, c, n, O=o, ws=ws))
+        elif kind == "rope_append":
+            x, c = _bf16(rows, (n_q + 2 * n_kv) * hd, dev), a_cache(ctx)
+            have, cu = torch.full((seqs,), prefix, dtype=torch.int32, device=dev), offsets(M)
+            tab = torch.rand((ctx, hd // 2, 2), device=dev)
+            q, k = torch.empty((rows, n_q * hd), dtype=torch.bfloat16, device=dev), torch.empty((rows, kv), dtype=torch.bfloat16, device=dev)
+            runs.append(lambda x=x, c=c, have=have, cu=cu, tab=tab, q=q, k=k, ws=ws: B.fpt_rope_append(
+                x, n_q, c, tab, have, cu_new=cu, Q=q, K=k, ws=ws))
+        else:
+            c, cu = a_cache(M), offsets(M)
+            k, v = (torch.empty((rows, kv), dtype=torch.bfloat16, device=dev) for _ in range(2))
+            runs.append(lambda c=c, cu=cu, k=k, v=v, ws=ws: B.fpt_kv_gather(c, cu, rows, K=k, V=v, ws=ws))
+    if kind == "attn_prompt":
+        return runs, 4.0 * seqs * n_q * hd * M * (prefix + (M + 1) / 2), 4.0 * rows * n_q * hd + 4.0 * seqs * ctx * kv
+    if kind == "attn_decode":
+        return runs, 4.0 * rows * n_q * hd, 2.0 * rows * kv + 4.0 * seqs * n_q * hd
+    if kind == "rope_append":
+        return runs, 0.0, rows * (4.0 * n_q * hd + 8.0 * kv) + 4.0 * rows * hd
+    return runs, 0.0, 6.0 * rows * kv
+
+
 def time_case(runs, reps, warmup=3):
     for i in range(max(warmup, 1)):
         runs[i % len(runs)]()
@@ -212,7 +262,8 @@ def main():
         return
     ap = argparse.ArgumentParser()
     ap.add_argument("kind", choices=["gemm", "act_quant", "silu_quant", "hadamard_quant", "linear", "mlp", "mlp_hadamard",
-                                     "gemm_a8", "act_quant_dynamic", "linear_dynamic", "attn_proj"])
+                                     "gemm_a8", "act_quant_dynamic", "linear_dynamic", "attn_proj",
+                                     "rope_append", "kv_gather", "attn_decode", "attn_prompt"])
     ap.add_argument("--M", type=int, default=2048)
     ap.add_argument("--N", type=int, default=4096)
     ap.add_argument("--K", type=int, default=4096)
@@ -222,10 +273,20 @@ def main():
     ap.add_argument("--f16-scales", action="store_true")
     ap.add_argument("--bits", type=int, default=4, help="activation bits of the dynamic kinds")
     ap.add_argument("--graph", action="store_true", help="replay the launches from a CUDA graph")
+    for name, default, what in (("--seqs", 1, "sequences of the attention calls, M tokens each"), ("--prefix", 0, "tokens before them"),
+                                ("--heads", 32, "query heads"), ("--kv-heads", 8, "key and value heads"), ("--head-dim", 128, None),
+                                ("--page", 64, "tokens of a cache page")):
+        ap.add_argument(name, type=int, default=default, help=what)
     a = ap.parse_args()
     B.lib()
     dev = torch.device("cuda", 0)
     torch.cuda.set_device(dev)
+    if a.kind in ("rope_append", "kv_gather", "attn_decode", "attn_prompt"):
+        runs, ops, nbytes = make_attn_case(a.kind, a.seqs, a.M, a.prefix, a.heads, a.kv_heads, a.head_dim, a.page, a.sets, dev)
+        us = time_case_graph(runs, a.reps, a.warmup) if a.graph else time_case(runs, a.reps, a.warmup)
+        print(json.dumps({"kind": a.kind, "seqs": a.seqs, "tokens": a.M, "prefix": a.prefix, "heads": [a.heads, a.kv_heads, a.head_dim],
+                          "sets": a.sets, "reps": a.reps, "us": us, "tops": ops / us / 1e6, "gbs": nbytes / us / 1e3}))
+        return
     runs, ops, nbytes = make_case(a.kind, a.M, a.N, a.K, a.sets, dev, a.f16_scales, a.bits)
     us = time_case_graph(runs, a.reps, a.warmup) if a.graph else time_case(runs, a.reps, a.warmup)
     print(json.dumps({"kind": a.kind, "M": a.M, "N": a.N, "K": a.K, "sets": a.sets, "reps": a.reps,

@@ -127,6 +127,23 @@ def test_binding_refuses_what_is_not_on_the_device():
             B.KVCache(*bad)
 
 
+def test_binding_refuses_what_is_no_tensor():
+    pages = torch.zeros((1, 2), dtype=torch.int32)
+    for bad in ((None,) * 5, (1, "k", None, 2.0, pages)):
+        with pytest.raises(ValueError):
+            B.KVCache(*bad)
+    c, x = B.KVCache.heads(2, 64), torch.zeros((1, 384), dtype=torch.bfloat16)
+    ws = torch.zeros(1 << 14, dtype=torch.uint8)
+    for call in (lambda: B.fpt_rope_append(None, 2, c, x, x, ws=ws), lambda: B.fpt_attn_decode(3, c, x, ws=ws),
+                 lambda: B.fpt_kv_gather(c, [0, 1], 1, ws=ws), lambda: B.fpt_attn_prompt("q", x, x, 2, 2, x, ws=ws),
+                 lambda: B.fpt_attn_prompt(x, x, x, 2, 2, x, ws=ws)):
+        with pytest.raises(B.FptError) as e:
+            call()
+        assert e.value.code == B.ERR_BAD_ARG
+    with pytest.raises(TypeError):
+        B._native().attn_decode(x)
+
+
 # ------------------------------------------------------------------------------------------------ tables
 def test_table_is_right_at_far_positions():
     import fractions

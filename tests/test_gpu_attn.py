@@ -775,3 +775,39 @@ def test_prompt_parts_captured_replayed_and_the_same_bits():
         assert torch.equal(out.view(torch.int16), first.view(torch.int16)) and torch.equal(lse, lse1)
         assert torch.equal(o.view(torch.int16), want.view(torch.int16))
     assert B.fpt_check_status(ws) == B.OK
+
+
+def test_calls_give_back_what_they_hold():
+    """Outputs are freed with the caller's references, those of refused calls at once; arguments keep their counts."""
+    import sys
+    rng = np.random.default_rng(53)
+    hd, page, n_q, n_kv = 64, 16, 4, 2
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, [40])
+    q, lens, ws = q.to(DEV), i32([40]), workspace()
+    x, tab, cu = bf16(rng, 1, (n_q + 2 * n_kv) * hd).to(DEV), torch.from_numpy(table(64, hd)).to(DEV), i32([0, 1])
+    kv = q[:, :n_kv * hd].contiguous()
+    args = (q, lens, ws, x, tab, cu, kv, cache.k, cache.ref)
+
+    def all_of_them():
+        B.fpt_attn_decode(q, cache, lens, want_lse=True, ws=ws)
+        B.fpt_attn_decode(q, cache, lens, O=kv.new_empty((1, n_q * hd)), ws=ws)
+        B.fpt_rope_append(x, n_q, cache, tab, lens, want_k=True, ws=ws)
+        B.fpt_kv_gather(cache, cu, 1, ws=ws)
+        B.fpt_attn_prompt(q, kv, kv, n_q, n_kv, cu, want_lse=True, ws=ws)
+        B.KVCache(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.pages)
+        for bad in (lambda: B.fpt_attn_decode(q, cache, lens, scale=-1.0, want_lse=True, ws=ws),
+                    lambda: B.fpt_attn_decode(q, cache, lens, O=q[:, :64], ws=ws),
+                    lambda: B.fpt_kv_gather(cache, cu, 1, V=q, ws=ws),
+                    lambda: B.fpt_attn_prompt(q, kv, kv, n_q, n_kv, cu, scale=0.0, want_lse=True, ws=ws)):
+            with pytest.raises(B.FptError):
+                bad()
+        with pytest.raises(TypeError):
+            B.fpt_attn_decode(q, cache, lens, scale="one", ws=ws)
+
+    B.set_allocator(None)                                # torch's own allocations are counted
+    all_of_them()
+    torch.cuda.synchronize()
+    counts, held = [sys.getrefcount(a) for a in args], torch.cuda.memory_allocated()
+    for _ in range(20):
+        all_of_them()
+    assert [sys.getrefcount(a) for a in args] == counts and torch.cuda.memory_allocated() == held
