@@ -66,6 +66,8 @@ struct DecSmem {
   static constexpr int kAlloc = kMiscOff + 16 + 1024;            // slack to align the base to 1024
 };
 
+constexpr int kDecWhole = 5;                       // see the producer warp's search
+
 // Row of the tile that stands at place l (0..15) of a 16-token group.
 __device__ __forceinline__ int token_row(int l) { return l ^ ((l & 1) << 2); }
 
@@ -145,12 +147,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   int first = 0, end = 0, off = 0, seq = 0;           // off: first tile of sequence `seq`
   Ranges ranges = {1, 0};
   if (warp == kDecWarps) {
-    int mine = 0;                                     // of the sequences lane, lane + 32, ...
+    int mine = 0, longest = 0;                        // of the sequences lane, lane + 32, ...
     bool bad = false;
     for (int s = lane; s < P.n_seqs; s += 32) {
       const int len = __ldg(P.kv_len + s);
       bad |= len < 0 || len > cap;
-      mine += tiles_of(min(len, cap)) * heads;
+      const int nt = tiles_of(min(len, cap));
+      longest = max(longest, nt);
+      mine += nt * heads;
     }
     auto scan = [&](int v) -> int {
 #pragma unroll
@@ -165,7 +169,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     if (bad && blockIdx.x == 0) record_bad_index(P.ws, kBadLength);
     ranges.each = total / ctas;
     ranges.longer = total - ranges.each * ctas;
-    if ((int)blockIdx.x < ctas) {
+    // Where there is a CTA for each row of tiles, and the longest is at most kDecWhole tiles longer than a range, rows stay whole: the join
+    // of parts takes longer than those tiles.  (32 heads, 8 of keys, of 128: 30 sequences of 400 tokens 17.7 -> 13.2 us, 50 of 600
+    // 24.0 -> 18.2; rows six tiles longer, 8 sequences of 400 tokens, 11.8 -> 12.6, eight longer 23.2 -> 24.4, so they are split.)
+    const int n_rows = P.n_seqs * heads, wanted = (int)blockIdx.x / heads;
+    const bool whole_rows = n_rows <= (int)gridDim.x && (int)__reduce_max_sync(0xffffffffu, (unsigned)longest) <= ranges.each + kDecWhole;
+    if ((int)blockIdx.x < (whole_rows ? n_rows : ctas)) {
       first = ranges.first_of(blockIdx.x);
       end = ranges.first_of(blockIdx.x + 1);
       for (int s0 = 0;; s0 += 32) {                   // (ends: the tiles add up to `total`)
@@ -174,11 +183,16 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           mine = s < P.n_seqs ? tiles_of(min(__ldg(P.kv_len + s), cap)) * heads : 0;
           incl = scan(mine);
         }
-        const uint32_t hit = __ballot_sync(0xffffffffu, off + incl > first);
+        const uint32_t hit = __ballot_sync(0xffffffffu, whole_rows ? s0 + lane == wanted : off + incl > first);
         if (hit) {
           const int src = __ffs(hit) - 1;
           off += __shfl_sync(0xffffffffu, incl - mine, src);
           seq = s0 + src;
+          if (whole_rows) {
+            const int nt = __shfl_sync(0xffffffffu, mine, src) / heads;
+            first = off + ((int)blockIdx.x - seq * heads) * nt;
+            end = first + nt;
+          }
           break;
         }
         off += __shfl_sync(0xffffffffu, incl, 31);

@@ -811,3 +811,22 @@ def test_calls_give_back_what_they_hold():
     for _ in range(20):
         all_of_them()
     assert [sys.getrefcount(a) for a in args] == counts and torch.cuda.memory_allocated() == held
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,n,most", [(128, 8, 2, 40, 300), (64, 1, 1, 100, 380), (128, 32, 2, 7, 65), (64, 12, 12, 33, 64), (128, 4, 4, 111, 700)])
+def test_decode_rows_kept_whole(hd, n_q, n_kv, n, most):
+    """A CTA for each row, short rows: nothing is joined; sequences looked at 32 at a time, empty ones, one too long for its pages."""
+    rng = np.random.default_rng(hd + n)
+    lens = [int(x) for x in rng.integers(0, most + 1, n)]
+    lens[0], lens[-1], lens[n // 2] = most, 1, 0
+    cache, pages, codes, scales, q = decode_case(rng, hd, 32, n_q, n_kv, lens)
+    ws = workspace()
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, 32, hd ** -0.5)
+    again = list(lens)
+    again[1] = 1 << 29
+    o2, _ = B.fpt_attn_decode(q.to(DEV), cache, i32(again), ws=ws)
+    assert B.fpt_check_status(ws) == B.ERR_INDEX
+    keep = [i for i in range(n) if i != 1]
+    check_decode(o2[keep], None, [lens[i] for i in keep], pages[keep], codes, scales, q[keep], n_q, hd, 32, hd ** -0.5)
