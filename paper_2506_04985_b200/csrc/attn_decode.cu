@@ -100,6 +100,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return d;
 }
 
+__device__ __forceinline__ uint32_t add_acq_rel(uint32_t* counter) {
+  uint32_t old;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+  return old;
+}
+
 // `total` tiles in `ctas` ranges: the first `longer` of them have each + 1 tiles, the others `each` (at least 1).
 struct Ranges {
   int each, longer;
@@ -111,6 +117,55 @@ struct Ranges {
 };
 
 __device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile : 1; }
+
+// Four elements, from d on, of the finished head h of a row.
+__device__ __forceinline__ void finish(__nv_bfloat16* O, float* lse, int hd, int h, int d, float4 o, float m, float sum) {
+  const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  *reinterpret_cast<uint2*>(O + h * hd + d) = make_uint2(f32x2_to_bf16x2_bits(o.x * inv, o.y * inv), f32x2_to_bf16x2_bits(o.z * inv, o.w * inv));
+  if (d == 0 && lse) lse[h] = sum > 0.0f || sum != sum ? (m - kDecLift) * 0.69314718055994531f + logf(sum) : -INFINITY;
+}
+
+// The join of a row's parts where they are few: each thread looks at all of them for four elements of a head, in one round of loads and
+// without a meeting.  (Not inlined: the main loop keeps its registers.)
+constexpr int kFew = 16;
+template <int HD, int NT>
+__device__ __noinline__ void join_few(const float* parts, int nparts, int gh, __nv_bfloat16* O, float* lse) {
+  constexpr int NH = 8 * NT, D4 = HD / 4;
+  auto part_at = [&](int p) { return parts + (size_t)(2 * p + (p == 0 ? 1 : 0)) * kAttnPartFloats; };
+#pragma unroll 1
+  for (int e = threadIdx.x; e < gh * D4; e += kDecWarps * 32) {
+    const int h = e / D4, d = (e % D4) * 4;
+    float m[kFew], l[kFew];
+#pragma unroll
+    for (int p = 0; p < kFew; ++p) {
+      const float* w = part_at(p < nparts ? p : 0) + NH * HD;
+      m[p] = p < nparts ? __ldcg(w + h) : -INFINITY;
+      l[p] = p < nparts ? __ldcg(w + NH + h) : 0.0f;
+    }
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int from = 0; from < kFew; from += 8) {
+      float4 x[8];
+#pragma unroll
+      for (int b = 0; b < 8; ++b)
+        x[b] = from + b < nparts ? __ldcg(reinterpret_cast<const float4*>(part_at(from + b) + (size_t)h * HD + d))
+                                 : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (from == 0) {
+#pragma unroll
+        for (int p = 0; p < kFew; ++p) top = fmaxf(top, m[p]);
+      }
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const float r = m[from + b] == -INFINITY ? 0.0f : ex2(m[from + b] - top);
+        sum = fmaf(l[from + b], r, sum);
+        o.x = fmaf(x[b].x, r, o.x); o.y = fmaf(x[b].y, r, o.y);
+        o.z = fmaf(x[b].z, r, o.z); o.w = fmaf(x[b].w, r, o.w);
+      }
+    }
+    finish(O, lse, HD, h, d, o, top, sum);
+  }
+}
 
 template <int HD, int NT, int ST, int MINB>
 __global__ void __launch_bounds__(kDecThreads, MINB)
@@ -552,12 +607,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int tid = threadIdx.x;
         const size_t q0 = (size_t)kvh * P.group + (size_t)blk * NH;        // first query head of the row
         auto emit = [&](int h, int d, float4 o, float m, float sum) {      // four elements of a finished head
-          const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-          uint2 w = make_uint2(f32x2_to_bf16x2_bits(o.x * inv, o.y * inv), f32x2_to_bf16x2_bits(o.z * inv, o.w * inv));
-          *reinterpret_cast<uint2*>(P.O + (size_t)row_seq * P.ld_o + (q0 + h) * HD + d) = w;
-          if (d == 0 && P.lse)
-            P.lse[(size_t)row_seq * P.n_q + q0 + h] =
-                sum > 0.0f || sum != sum ? (m - kDecLift) * 0.69314718055994531f + logf(sum) : -INFINITY;
+          finish(P.O + (size_t)row_seq * P.ld_o + q0 * HD, P.lse ? P.lse + (size_t)row_seq * P.n_q + q0 : nullptr, HD, h, d, o, m, sum);
         };
         constexpr int D4 = HD / 4, kPerThread = NH * D4 / (kDecWarps * 32);
         float* part = P.parts + (size_t)(2 * (int)blockIdx.x + ((int)blockIdx.x == part0 ? 1 : 0)) * kAttnPartFloats;
@@ -586,11 +636,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         if (!(flags & 4)) {
           if (!meet()) break;
           if (tid == 0) {
-            __threadfence();                            // (the whole CTA's part, which the warps' meeting put before this)
+            // (releases the whole CTA's part, which the warps' meeting put before this, and acquires the others')
             uint32_t* counter = P.ws + kCounterWord0 + part0;
-            const bool last = atomicAdd(counter, 1u) == (uint32_t)nparts - 1u;
+            const bool last = add_acq_rel(counter) == (uint32_t)nparts - 1u;
             if (last) *counter = 0;                   // as the next call finds it
-            __threadfence();
             *last_flag = last;
           }
           if (!meet()) break;
@@ -599,10 +648,14 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             // exponents (a head and every 128 / NH-th part a thread), then weights into shared memory, as many parts at a time as it
             // has room for, then the sums: loads of one step do not wait for one another.
             auto part_at = [&](int p) { return P.parts + (size_t)(2 * (part0 + p) + (p == 0 ? 1 : 0)) * kAttnPartFloats; };
+            constexpr int kStep = kDecWarps * 32 / NH, kBatch = 12;
+            if (nparts <= kFew) {
+              join_few<HD, NT>(P.parts + (size_t)(2 * part0) * kAttnPartFloats, nparts, gh, P.O + (size_t)row_seq * P.ld_o + q0 * HD,
+                               P.lse ? P.lse + (size_t)row_seq * P.n_q + q0 : nullptr);
+            } else {
             constexpr int kRoom = kDecWarps * HD;       // parts whose weights fit
             float* weights = merge;                     // [part][NH]
             const int h0 = tid % NH, p0 = tid / NH;
-            constexpr int kStep = kDecWarps * 32 / NH, kBatch = 12;
             float top = -INFINITY;
             // (a batch of loads has a fixed length, what lies behind the last part left out: the tail of an unrolled loop would
             // wait for one load after the other, 6 us of 11 with 55 parts)
@@ -681,6 +734,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                 for (int i = 0; i < kStep; ++i) all += merge[i * NH + h];
                 emit(h, d, o[k], merge[kDecWarps * 32 + h], all);
               }
+            }
             }
           }
         }
