@@ -224,11 +224,11 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     if (bad && blockIdx.x == 0) record_bad_index(P.ws, kBadLength);
     ranges.each = total / ctas;
     ranges.longer = total - ranges.each * ctas;
-    // Where there is a CTA for each row of tiles, and the longest is at most kDecWhole tiles longer than a range, rows stay whole: the join
-    // of parts takes longer than those tiles.  (32 heads, 8 of keys, of 128: 30 sequences of 400 tokens 17.7 -> 13.2 us, 50 of 600
-    // 24.0 -> 18.2; rows six tiles longer, 8 sequences of 400 tokens, 11.8 -> 12.6, eight longer 23.2 -> 24.4, so they are split.)
+    // Where there is a CTA for each row of tiles, and the longest has not many more tiles than a range, rows stay whole: the join of parts
+    // takes longer than those tiles.  (32 heads, 8 of keys, of 128: 30 sequences of 400 tokens, seven tiles against three, 16.2 -> 13.9 us,
+    // 50 of 600 22.7 -> 18.2; one of 200, four against one, 7.7 -> 8.3, 30 of 1000, 16 against eight, 21.6 -> 24.4: those are split.)
     const int n_rows = P.n_seqs * heads, wanted = (int)blockIdx.x / heads;
-    const bool whole_rows = n_rows <= (int)gridDim.x && (int)__reduce_max_sync(0xffffffffu, (unsigned)longest) <= ranges.each + kDecWhole;
+    const bool whole_rows = n_rows <= (int)gridDim.x && (int)__reduce_max_sync(0xffffffffu, (unsigned)longest) <= ranges.each + min(ranges.each + 1, kDecWhole);
     if ((int)blockIdx.x < (whole_rows ? n_rows : ctas)) {
       first = ranges.first_of(blockIdx.x);
       end = ranges.first_of(blockIdx.x + 1);

@@ -813,7 +813,8 @@ def test_calls_give_back_what_they_hold():
     assert [sys.getrefcount(a) for a in args] == counts and torch.cuda.memory_allocated() == held
 
 
-@pytest.mark.parametrize("hd,n_q,n_kv,n,most", [(128, 8, 2, 40, 300), (64, 1, 1, 100, 380), (128, 32, 2, 7, 65), (64, 12, 12, 33, 64), (128, 4, 4, 111, 700)])
+@pytest.mark.parametrize("hd,n_q,n_kv,n,most", [(128, 8, 2, 40, 300), (64, 1, 1, 100, 380), (128, 32, 2, 7, 65), (64, 12, 12, 33, 64), (128, 4, 4, 111, 700),
+                                                   (128, 8, 2, 40, 190), (64, 1, 1, 100, 190)])
 def test_decode_rows_kept_whole(hd, n_q, n_kv, n, most):
     """A CTA for each row, short rows: nothing is joined; sequences looked at 32 at a time, empty ones, one too long for its pages."""
     rng = np.random.default_rng(hd + n)
