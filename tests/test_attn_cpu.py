@@ -257,3 +257,26 @@ def test_ranges_of_tiles():
         for x in rng.integers(0, total, 20):
             c = x // (each + 1) if x < edge else longer + (x - edge) // each
             assert first[c] <= x < first[c + 1]
+
+
+# ------------------------------------------------------------------------------------------------ the source
+def test_whole_warps_leave_a_wait_as_one():
+    """As in test_waits_cpu.py, for the attention kernels: only the thread that issues the prompt kernel's matrix instructions (roles 2
+    and 3 there) waits alone, and nothing waits without a limit."""
+    import glob
+    import os
+    import re
+    here = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2506_04985_b200", "csrc")
+    seen = 0
+    for path in sorted(glob.glob(os.path.join(here, "attn_*.cu"))):
+        text = open(path).read()
+        name = os.path.basename(path)
+        for whole, role in re.findall(r"\bwait_long<(true|false)>\([^;{]*?, (\d+)\)", text):
+            seen += 1
+            assert (whole == "false") == (name == "attn_prompt.cu" and int(role) in (2, 3)), (name, whole, role)
+        assert text.count("wait_long<") == len(re.findall(r"\bwait_long<(?:true|false)>\([^;{]*?, \d+\)", text)), name
+        for line in text.splitlines():
+            if "mbar_try_wait(" in line:
+                assert "globaltimer_ns() - t0 <" in line, (name, line)
+        assert "bar.sync" not in text and "__trap" not in text
+    assert seen >= 20
