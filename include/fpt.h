@@ -410,7 +410,7 @@ typedef struct fpt_kv_cache {
  *        new codes  clamp(rne(v * inv), -127, 127), infinities end at the clamp, a NaN gives -127
  *        held codes clamp(rne(q * (s_old * inv)), -127, 127) where s > s_old
  *     so a page's scale grows with its tokens and never shrinks while it keeps one (tokens taken back by a smaller ctx
- *     keep their part in it).  A page that a call writes belongs to one sequence.
+ *     keep their part in it).  A page that a call writes belongs to one sequence and stands once in its row of pages.
  */
 int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int n_q,
                     const float* rope, int n_pos, int rot_dim, int layout,
