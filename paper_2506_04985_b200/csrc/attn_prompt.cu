@@ -83,10 +83,10 @@ struct PrSmem {
   static constexpr int kHalf = kPrTile * 128;                // 64 of its columns: 128-byte rows
   static constexpr int kKvOff = 2 * kMat;
   static constexpr int kBarOff = kKvOff + kStages * kMat;
-  static constexpr int kNumBars = 4 + 4 * kStages + 2 * 13 + 1;
+  static constexpr int kNumBars = 4 + 4 * kStages + 30 + 1;
   static constexpr int kMiscOff = (kBarOff + kNumBars * 8 + 15) / 16 * 16;
   static constexpr int kInfoOff = kMiscOff + 32;             // (16 bytes of misc, the answer of the launch control)
-  static constexpr int kStatOff = kInfoOff + 2 * 64;         // [query tile][row] {maximum, sum of weights}
+  static constexpr int kStatOff = kInfoOff + 4 * (int)sizeof(TaskInfo);         // [query tile][row] {maximum, sum of weights}
   static constexpr int kAlloc = kStatOff + 2 * kPrTile * 8;
 };
 
@@ -222,21 +222,23 @@ __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane)
       }
     }
     if (P.n_seqs <= 32) {
-      const uint32_t n = SPLIT ? __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0]) : 0, most = SPLIT ? (uint32_t)(P.split / P.units) : 0;
-      if (n < most) {                                        // (fewer than the SMs, and below 2^24 tiles each: no overflow)
-        const uint32_t tiles = (uint32_t)(max(keys, 0) + kPrTile - 1) / kPrTile;
-        const uint32_t all = __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0] * tiles);
-        const uint32_t least = max((uint32_t)kPrPartTiles, (all + (most - n) - 1) / (most - n));
-        if (tiles > least) o.parts = (int)min((tiles + least - 1) / least, (uint32_t)kPrParts);
-        o.count[0] *= o.parts;
-        o.slot = o.parts > 1 ? o.count[0] : 0;
-        int v = o.slot;
-#pragma unroll
-        for (int k = 1; k < 32; k <<= 1) {
-          const int u = __shfl_up_sync(0xffffffffu, v, k);
-          if (lane >= k) v += u;
+      if constexpr (SPLIT) {
+        const uint32_t n = __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0]), most = (uint32_t)(P.split / P.units);
+        if (n < most) {                                      // (fewer than the SMs, and below 2^24 tiles each: no overflow)
+          const uint32_t tiles = (uint32_t)(max(keys, 0) + kPrTile - 1) / kPrTile;
+          const uint32_t all = __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0] * tiles);
+          const uint32_t least = max((uint32_t)kPrPartTiles, (all + (most - n) - 1) / (most - n));
+          if (tiles > least) o.parts = (int)min((tiles + least - 1) / least, (uint32_t)kPrParts);
+          o.count[0] *= o.parts;
+          o.slot = o.parts > 1 ? o.count[0] : 0;
+          int v = o.slot;
+  #pragma unroll
+          for (int k = 1; k < 32; k <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, v, k);
+            if (lane >= k) v += u;
+          }
+          o.slot = v - o.slot;
         }
-        o.slot = v - o.slot;
       }
       for (int k = 0; k < P.n_seqs; ++k) {
         const int other = __shfl_sync(0xffffffffu, keys, k), c = __shfl_sync(0xffffffffu, o.count[i], k);
@@ -458,10 +460,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   auto o_full = [&](int w) { return bar1 + 8u * (14 + w); };                       // a task's last P V
   auto o_empty = [&](int w) { return bar1 + 8u * (16 + w); };
   auto info_full = [&](int i) { return bar1 + 8u * (18 + i); };
-  auto info_empty = [&](int i) { return bar1 + 8u * (20 + i); };
-  auto stat_full = [&](int w) { return bar1 + 8u * (22 + w); };
-  auto stat_empty = [&](int w) { return bar1 + 8u * (24 + w); };
-  const uint32_t answered = bar1 + 8u * 26;
+  auto info_empty = [&](int i) { return bar1 + 8u * (22 + i); };
+  auto stat_full = [&](int w) { return bar1 + 8u * (26 + w); };
+  auto stat_empty = [&](int w) { return bar1 + 8u * (28 + w); };
+  const uint32_t answered = bar1 + 8u * 30;
   float2* stats = reinterpret_cast<float2*>(smem + L::kStatOff);
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + L::kMiscOff);
   volatile uint32_t* abort_flag = misc + 1;
@@ -484,11 +486,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       for (int b = 0; b < 4; ++b) mbar_init(p_full(i, b >> 1, b & 1), 4);
       mbar_init(o_full(i), 1);
       mbar_init(o_empty(i), 4);
-      mbar_init(info_full(i), 1);
-      mbar_init(info_empty(i), 8 + 4 + 1 + 2);
       mbar_init(stat_full(i), 4);
       mbar_init(stat_empty(i), 4);
     }
+    for (int i = 0; i < 4; ++i) { mbar_init(info_full(i), 1); mbar_init(info_empty(i), 8 + 4 + 1 + 2); }
     mbar_init(answered, 1);
     for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), 1); mbar_init(kv_empty(i), 1); mbar_init(v_raw(i), 1); mbar_init(v_clean(i), 2); }
     misc[1] = 0;
@@ -524,14 +525,14 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint32_t step = 0, stat_ph = 0;                           // step: of this tile in all tasks
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 7)) break;
-      const TaskInfo* info = infos + (n & 1);
+      if (!wait_long<true>(info_full(n & 3), (n >> 2) & 1, abort_flag, P.status, 7)) break;
+      const TaskInfo* info = infos + (n & 3);
       const int flags = info->flags, tiles = info->tiles, plain = min(info->cut, tiles);
       // keys the row sees (not fewer in the rows behind it, those behind the sequence among them)
       const int limit = (P.causal ? max(0, min(info->len_k, info->tok0 + w * per_tile + (r >> P.pack_log2) + (info->len_k - info->len_q) + 1))
                                   : info->len_k) - (SPLIT ? info->skip : 0);
       __syncwarp();
-      if (lane == 0) mbar_arrive(info_empty(n & 1));
+      if (lane == 0) mbar_arrive(info_empty(n & 3));
       if (!(flags & 1)) break;
       if (w == 1 && !(flags & 2)) continue;
       int place = w;
@@ -638,8 +639,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     const int pack_mask = (1 << P.pack_log2) - 1;
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 9)) break;
-      const volatile TaskInfo* info = infos + (n & 1);
+      if (!wait_long<true>(info_full(n & 3), (n >> 2) & 1, abort_flag, P.status, 9)) break;
+      const volatile TaskInfo* info = infos + (n & 3);
       if (!(info->flags & 1)) break;
       const int tiles = info->tiles, len_q = info->len_q, row0 = info->row0, head0 = info->head0;
       const bool split = SPLIT && info->parts > 1;
@@ -704,7 +705,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               sum > 0.0f || sum != sum ? ms.x * 0.69314718055994531f + logf(sum) : -INFINITY;
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(info_empty(n & 1));         // (at the end: `odd` comes late)
+      if (lane == 0) mbar_arrive(info_empty(n & 3));         // (at the end: `odd` comes late)
     }
   } else {
     reg_dec<kPrAuxRegs>();
@@ -740,10 +741,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         TaskInfo ti = {};
         const bool found = bid >= 0 && find_prompt_task<SPLIT>(P, order, bid, lane, ti);
         if (found || bid < 0) {
-          if (!wait_long<true>(info_empty(n & 1), ((n >> 1) & 1) ^ 1u, abort_flag, P.status, 1)) { ok = false; break; }
+          if (!wait_long<true>(info_empty(n & 3), ((n >> 2) & 1) ^ 1u, abort_flag, P.status, 1)) { ok = false; break; }
           if (lane == 0) {
-            infos[n & 1] = ti;
-            mbar_arrive(info_full(n & 1));
+            infos[n & 3] = ti;
+            mbar_arrive(info_full(n & 3));
           }
           ++n;
           if (bid < 0) break;
@@ -807,10 +808,10 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           return got;
         };
         for (int n = 0; ok; ++n) {
-          if (!wait_long<false>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 2)) break;
-          const volatile TaskInfo* info = infos + (n & 1);
+          if (!wait_long<false>(info_full(n & 3), (n >> 2) & 1, abort_flag, P.status, 2)) break;
+          const volatile TaskInfo* info = infos + (n & 3);
           const int flags = info->flags, tiles = info->tiles, cut = info->cut;
-          mbar_arrive(info_empty(n & 1));
+          mbar_arrive(info_empty(n & 3));
           if (!(flags & 1)) break;
           if (tiles == 0) continue;
           const int nw = (flags & 2) ? 2 : 1;
@@ -876,8 +877,8 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       uint32_t raw_par = 0;
       int first = 1;                                          // place in the ring of the task's first values
       for (int n = 0;; ++n) {
-        if (!wait_long<true>(info_full(n & 1), (n >> 1) & 1, abort_flag, P.status, 6)) break;
-        TaskInfo* info = infos + (n & 1);
+        if (!wait_long<true>(info_full(n & 3), (n >> 2) & 1, abort_flag, P.status, 6)) break;
+        TaskInfo* info = infos + (n & 3);
         const int flags = info->flags, tiles = info->tiles, cut = info->cut, len_k = info->len_k - (SPLIT ? info->skip : 0);
         bool ok = true;
         for (int j = cut; ok && j < tiles; ++j) {
@@ -925,7 +926,7 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
         first = (first + 2 * tiles) % ST;
         __syncwarp();
-        if (lane == 0) mbar_arrive(info_empty(n & 1));
+        if (lane == 0) mbar_arrive(info_empty(n & 3));
         if (!ok || !(flags & 1)) break;
       }
     }
