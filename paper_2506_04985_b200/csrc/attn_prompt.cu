@@ -192,7 +192,7 @@ __device__ __forceinline__ int block_of_answer(uint32_t answer) {
 constexpr int kPrHeld = 4;
 constexpr int kPrPartTiles = 4, kPrParts = 32;       // a part's tiles at the least, a task's parts at the most
 constexpr int kPrSplitGain = 6;                        // tiles less to walk through for which keys are split
-struct TaskOrder { int first[kPrHeld], count[kPrHeld], parts, slot; };
+struct TaskOrder { int first[kPrHeld], count[kPrHeld], q0[kPrHeld], len_q[kPrHeld], k0[kPrHeld], len_k[kPrHeld], parts, slot; };
 //
 // Few query rows and many keys leave SMs idle: the keys of up to 32 sequences are then split, so that the tasks are at most as many as
 // the SMs (and as the workspace holds sums of).  With N tasks of t_i tiles, parts of L tiles are ceil(t_i / L) <= t_i / L + 1 tasks each,
@@ -207,8 +207,7 @@ __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane)
   o.slot = 0;
 #pragma unroll
   for (int i = 0; i < kPrHeld; ++i) {
-    o.first[i] = 0;
-    o.count[i] = 0;
+    o.first[i] = o.count[i] = o.q0[i] = o.len_q[i] = o.k0[i] = o.len_k[i] = 0;
     const int s = lane + 32 * i;
     if (P.n_seqs > 32 * kPrHeld || 32 * i >= P.n_seqs) continue;
     int keys = -1;
@@ -218,6 +217,7 @@ __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane)
         record_bad_index(P.status, kBadOffset);
       } else {
         keys = k1 - k0;
+        o.q0[i] = q0; o.len_q[i] = q1 - q0; o.k0[i] = k0; o.len_k[i] = keys;
         o.count[i] = (q1 - q0 + ((256 >> P.pack_log2) - 1)) >> (8 - P.pack_log2);
       }
     }
@@ -276,6 +276,10 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
         const int l = __ffs(mine) - 1;
         lo = l + 32 * i;
         place = __shfl_sync(0xffffffffu, order.first[i] + order.count[i], l) - 1 - turn;      // last rows first
+        ti.row0 = __shfl_sync(0xffffffffu, order.q0[i], l);
+        ti.len_q = __shfl_sync(0xffffffffu, order.len_q[i], l);
+        ti.key0 = __shfl_sync(0xffffffffu, order.k0[i], l);
+        ti.len_k = __shfl_sync(0xffffffffu, order.len_k[i], l);
         if (SPLIT && i == 0) {
           parts = __shfl_sync(0xffffffffu, order.parts, l);
           slot = __shfl_sync(0xffffffffu, order.slot, l);
@@ -293,22 +297,22 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
       hi = min(hi, lo + step);
     }
     place = id - ((__ldg(P.cu_q + lo) >> per_log2) + lo);
+    ti.row0 = __ldg(P.cu_q + lo);
+    const int end_q = __ldg(P.cu_q + lo + 1);
+    ti.len_q = end_q - ti.row0;
+    ti.key0 = __ldg(P.cu_k + lo);
+    const int end_k = __ldg(P.cu_k + lo + 1);
+    ti.len_k = end_k - ti.key0;
+    if (ti.row0 < 0 || end_q < ti.row0 || end_q > P.M_q || ti.key0 < 0 || end_k < ti.key0 || end_k > P.M_k) {
+      if (lane == 0) record_bad_index(P.status, kBadOffset);
+      return false;
+    }
   }
   if (SPLIT && parts > 1) {
     const int whole = place / parts;
     ti.part = place - whole * parts;
     place = whole;
     ti.slot = (slot + place * parts) * P.units + unit * parts;
-  }
-  ti.row0 = __ldg(P.cu_q + lo);
-  const int end_q = __ldg(P.cu_q + lo + 1);
-  ti.len_q = end_q - ti.row0;
-  ti.key0 = __ldg(P.cu_k + lo);
-  const int end_k = __ldg(P.cu_k + lo + 1);
-  ti.len_k = end_k - ti.key0;
-  if (ti.row0 < 0 || end_q < ti.row0 || end_q > P.M_q || ti.key0 < 0 || end_k < ti.key0 || end_k > P.M_k) {
-    if (lane == 0) record_bad_index(P.status, kBadOffset);
-    return false;
   }
   if (place < 0 || place >= (ti.len_q + per - 1) >> per_log2) return false;
   ti.tok0 = place * per;
