@@ -71,16 +71,18 @@ __device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435
 // sequence s, rows cu[s] .. cu[s+1]-1, is given floor(cu[s+1] / block) - floor(cu[s] / block) + 2 tasks, which
 // is at least the number of blocks that its rows can touch, and task `id` belongs to the s whose tasks it is among.  All sequences are looked at
 // side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the look: one round of
-// loads, where a binary search would wait for one load after the other.
+// loads, where a binary search would wait for one load after the other.  block 0: a task for each row, place 0.
 struct FoundTask { int seq, place, row0, rows, extra; };
-__device__ __forceinline__ FoundTask find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int block,
+__device__ __forceinline__ FoundTask find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int M, int block,
                                                int id, FoundTask* found /* shared */, uint32_t* status) {
   if (threadIdx.x == 0) found->seq = -1;
   __syncthreads();
   for (int s = threadIdx.x; s < n_seqs; s += blockDim.x) {
     const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1), e = extra ? __ldg(extra + s) : 0;
-    if (lo < 0 || hi < lo) {
+    if (lo < 0 || hi < lo || hi > M) {
       if (blockIdx.x == 0) record_bad_index(status, kBadOffset);
+    } else if (block == 0) {
+      if (lo <= id && id < hi) *found = FoundTask{s, 0, lo, hi - lo, e};
     } else {
       const int a = lo / block + 2 * s;
       if (a <= id && id < hi / block + 2 * s + 2) *found = FoundTask{s, id - a, lo, hi - lo, e};

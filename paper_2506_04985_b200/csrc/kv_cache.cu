@@ -23,7 +23,7 @@ struct RopeParams {
   float *k_scale, *v_scale;
   __nv_bfloat16 *Qo, *Ko;
   uint32_t* status;
-  int M, ld, ld_q, ld_k, n_q, n_kv, n_pos, rot, interleaved, n_seqs, n_pages, page, max_pages;
+  int M, ld, ld_q, ld_k, n_q, n_kv, n_pos, rot, interleaved, n_seqs, n_pages, page, max_pages, by_row;
 };
 
 // Sixteen elements of a head: two runs of eight, at `a` and at `b`.  Neighbours' runs follow each other (16 bytes a lane at a
@@ -131,21 +131,22 @@ __global__ void __launch_bounds__(T, (N <= 2 ? 1024 : 512) / T) rope_append_kern
   pdl_launch_dependents();
 
   const int head = blockIdx.y % P.n_kv, tid = threadIdx.x;
-  const FoundTask task = P.cu ? find_task(P.cu, P.ctx, P.n_seqs, P.page, blockIdx.x, &found, P.status)
+  const FoundTask task = P.cu ? find_task(P.cu, P.ctx, P.n_seqs, P.M, P.by_row ? 0 : P.page, blockIdx.x, &found, P.status)
                               : FoundTask{(int)blockIdx.x, 0, (int)blockIdx.x, 1, __ldg(P.ctx + blockIdx.x)};
-  const int s = task.seq, place = task.place, row0 = task.row0, n_new = task.rows, ctx = task.extra;
+  const int s = task.seq, row0 = task.row0, n_new = task.rows, ctx = task.extra;
   if (s < 0) return;
-  if (row0 > P.M - n_new) {                     // (both are at least 0)
-    if (tid == 0) record_bad_index(P.status, kBadOffset);
-    return;
-  }
   if (ctx < 0 || ctx > P.n_pos - n_new) {       // a position without a rotation
     if (tid == 0 && n_new > 0) record_bad_index(P.status, kBadPosition);
     return;
   }
   // without a cache the pages are blocks of rows, counted from the sequence's first
   const int base = P.k ? ctx : 0;
-  const int page_no = base / P.page + place;
+  int page_no = base / P.page + task.place;
+  if (P.by_row) {                               // the first of the sequence's rows in a page has the page
+    const int at = base + ((int)blockIdx.x - row0);
+    if (at != base && at % P.page) return;
+    page_no = at / P.page;
+  }
   const int lo = max(base, page_no * P.page), hi = min(base + n_new, (page_no + 1) * P.page);
   if (lo >= hi) return;
   const int n = hi - lo;                        // new tokens of this page
@@ -312,10 +313,10 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams P) {
   __shared__ FoundTask found;
   pdl_wait();
   pdl_launch_dependents();
-  const FoundTask task = find_task(P.cu, P.first, P.n_seqs, P.page, blockIdx.x, &found, P.status);
+  const FoundTask task = find_task(P.cu, P.first, P.n_seqs, P.M, P.page, blockIdx.x, &found, P.status);
   const int s = task.seq, place = task.place, row0 = task.row0, n_rows = task.rows, first = task.extra, tid = threadIdx.x;
   if (s < 0) return;
-  if (row0 > P.M - n_rows || first < 0 || first > INT32_MAX - 1024 - n_rows) {
+  if (first < 0 || first > INT32_MAX - 1024 - n_rows) {
     if (tid == 0) record_bad_index(P.status, kBadOffset);
     return;
   }
@@ -419,7 +420,11 @@ extern "C" int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int
     P.n_pages = cache->n_pages; P.page = cache->page; P.max_pages = cache->max_pages;
   }
   cudaStream_t st = (cudaStream_t)stream;
-  const int64_t tasks = cu_new ? (int64_t)M / P.page + 2 * (int64_t)n_seqs : n_seqs;
+  // The pages that the rows may touch, numbered without their lengths; few rows a sequence: a task for each row, of which the first in a page
+  // works (64 sequences of one token, 16 CTAs a task: 7.6 -> 5.7 us).
+  const int64_t by_page = (int64_t)M / P.page + 2 * (int64_t)n_seqs;
+  P.by_row = cu_new && M < by_page;
+  const int64_t tasks = !cu_new ? n_seqs : P.by_row ? M : by_page;
   if (tasks > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   // one token a sequence: its heads' pieces are few, and what a CTA has to do beside them is to round the page's held tokens
   // again where its scale grows; otherwise a page a CTA

@@ -831,3 +831,33 @@ def test_decode_rows_kept_whole(hd, n_q, n_kv, n, most):
     assert B.fpt_check_status(ws) == B.ERR_INDEX
     keep = [i for i in range(n) if i != 1]
     check_decode(o2[keep], None, [lens[i] for i in keep], pages[keep], codes, scales, q[keep], n_q, hd, 32, hd ** -0.5)
+
+
+FEW_ROWS = [
+    # hd, page, n_q, n_kv, rot, interleaved, new, ctx: less than two rows a sequence
+    (128, 64, 8, 2, 128, 0, [1] * 20 + [0] * 5 + [9, 2], [(37 * i) % 130 for i in range(25)] + [60, 63]),
+    (64, 16, 4, 4, 64, 1, [0] * 7 + [40] + [0] * 30 + [1, 3], [5] * 7 + [10] + [0] * 30 + [15, 14]),
+    (128, 128, 2, 1, 64, 0, [2, 0, 1, 0, 0, 2], [127, 3, 128, 0, 9, 126]),
+]
+
+
+@pytest.mark.parametrize("hd,page,n_q,n_kv,rot,inter,new,ctx", FEW_ROWS)
+def test_append_of_few_rows_a_sequence(hd, page, n_q, n_kv, rot, inter, new, ctx):
+    test_append_matches_the_oracle_bit_for_bit(hd, page, n_q, n_kv, rot, inter, new, ctx, False)
+
+
+def test_few_rows_turned_without_a_cache_and_offsets_out_of_range():
+    rng = np.random.default_rng(54)
+    hd, n_q, n_kv, new = 64, 4, 2, [0, 2, 1, 0, 1, 3]
+    rows, ctx = sum(new), [3, 9, 0, 4, 63, 64]
+    x, tab, ws = bf16(rng, rows, (n_q + 2 * n_kv) * hd), table(70, hd), workspace()
+    tabd, cu = torch.from_numpy(tab).to(DEV), offsets(new)
+    q, k = B.fpt_rope_append(x.to(DEV), n_q, B.KVCache.heads(n_kv, hd), tabd, i32(ctx), cu_new=i32(cu.tolist()), want_k=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    at = np.concatenate([np.arange(c, c + n) for c, n in zip(ctx, new)])
+    want = OA.rope(x.float().numpy().reshape(rows, -1, hd)[:, :n_q + n_kv], tab[at], hd, False)
+    assert np.array_equal(bf16_host(q), want[:, :n_q].reshape(rows, -1)) and np.array_equal(bf16_host(k), want[:, n_q:].reshape(rows, -1))
+    for bad in ([9, 9, 9, 9, 9, 9, 12], [0, 2, 3, 3, 4, 7, 8], [-1, 0, 0, 0, 0, 0, 0], [0, 3, 1, 1, 1, 1, 1]):
+        ws = workspace()
+        B.fpt_rope_append(x.to(DEV), n_q, B.KVCache.heads(n_kv, hd), tabd, i32(ctx), cu_new=i32(bad), ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX, bad
