@@ -861,3 +861,20 @@ def test_few_rows_turned_without_a_cache_and_offsets_out_of_range():
         ws = workspace()
         B.fpt_rope_append(x.to(DEV), n_q, B.KVCache.heads(n_kv, hd), tabd, i32(ctx), cu_new=i32(bad), ws=ws)
         assert B.fpt_check_status(ws) == B.ERR_INDEX, bad
+
+
+PADDED = [
+    # hd, n_q, n_kv, len_q, len_k (None: the same), causal: groups that no power of two divides, short sequences
+    (128, 40, 8, [9, 6, 1, 14, 0, 11], None, True),
+    (64, 20, 4, [78, 19, 51], [90, 19, 333], True),
+    (128, 14, 2, [1, 1, 1], [700, 3, 130], True),
+    (64, 36, 3, [13, 16, 2], None, True),
+    (128, 19, 1, [7, 5], [64, 200], False),
+    (64, 3, 1, [1], [9000], True),                           # one head of padding, keys in parts
+    (128, 10, 2, [12], [3000], True),
+]
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,len_q,len_k,causal", PADDED)
+def test_prompt_heads_that_fill_no_tile(hd, n_q, n_kv, len_q, len_k, causal):
+    test_prompt(hd, n_q, n_kv, len_q, len_k, causal)
