@@ -21,6 +21,9 @@
 // Softmax in the exponent of two: p = 2^(S scale log2(e) - m).  m is the row's maximum when it was last renewed: it is renewed, and O in
 // tensor memory multiplied by 2^(m_old - m_new), only where the maximum has grown by more than 8, so that p <= 256; the quotient by
 // the sum of weights is the same for any m.
+// Measured (32 query heads, 8 of keys, of 128): 2048 tokens 36.7 us, 8192 442 us = 1.24 PFLOP/s, 490 to 510 us once the GPU is hot (power, 1.64 GHz).  A
+// pair of tiles and 128 keys take 3 270 cycles, of which the tensor core works 2 150: what bounds it is the chain from scores to
+// committed weights, not a unit.
 // (A part of the powers as a polynomial on the multiply-add units, since 128 powers a row keep the special-function unit busy half
 // as long as the tensor core works on a tile: 3 % slower at a quarter of them, 13 % at half.)
 #include <algorithm>
