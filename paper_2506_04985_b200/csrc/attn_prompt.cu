@@ -1,7 +1,7 @@
 // Causal attention of packed prompts (fpt_attn_prompt; formulas: include/fpt.h).
 //
 // A task is two tiles of 128 query rows of one key/value head, and a walk over that head's keys in tiles of 128.  A row
-// is a (token, query head of the group) pair: as many heads of the group as divide 128 share a tile, so a prompt of few
+// is a (token, query head of the group) pair: a power of two of the heads of a group share a tile, so a prompt of few
 // tokens still fills it, and the keys are fetched once for all of them.  The grid has a CTA a task, in the order of a sequence's
 // last rows first (with a causal mask, the longest); a CTA that has requested all of its task's keys takes over one that was
 // not started yet (cluster launch control), so that the loads, the look-ups and the first scores of the next task run under the last
