@@ -75,7 +75,7 @@ struct PromptParams {
   uint32_t* status;
   float* sums;                        // of parts
   int ld_v, ld_o, M_q, M_k, n_q, n_kv, group, pack_log2, packs, units, n_seqs, n_tasks, causal;
-  int split;                          // tasks, parts counted, that are at most made where keys are split; 0: they are not
+  int split, sms;                     // parts that are at most made where keys are split; SMs.  0: they are not
   float scale_log2;
 };
 
@@ -191,24 +191,50 @@ __device__ __forceinline__ int block_of_answer(uint32_t answer) {
   return x;
 }
 
-// Where the tasks of up to 128 sequences begin and how many they are: lane l knows it of sequences l, l + 32, ...  Up to 32 are
-// taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short; more as they come.
 constexpr int kPrHeld = 4;
 constexpr int kPrPartTiles = 4, kPrParts = 32;       // a part's tiles at the least, a task's parts at the most
 constexpr int kPrSplitGain = 6;                        // tiles less to walk through for which keys are split
-struct TaskOrder { int first[kPrHeld], count[kPrHeld], q0[kPrHeld], len_q[kPrHeld], k0[kPrHeld], len_k[kPrHeld], parts, slot; };
+
+// The tasks of one sequence with more tiles of keys than L, which are its last ones, in equal parts of at most L tiles.  L is a quarter more
+// than an SM's share of all tiles, at least kPrPartTiles, and as much more as it takes for the workspace to hold the parts' sums.
+// (32 heads of 128 and 8 of keys: 64 queries behind 4 000 keys 62 -> 29 us, 256 behind 30 000 409 -> 163; 16 behind
+// 100 000, 8 heads: 1 197 -> 71; one prompt of 5 400, 5 heads and one of keys, 83 -> 62; of 4 000, 4 heads, 60 -> 43.)
+struct Splitting {
+  int len_k, len_q, places, per_log2, causal;                // places: tasks a unit
+  __host__ __device__ int most() const { return (int)(((uint32_t)len_k + kPrTile - 1) / kPrTile); }
+  // all its tasks' tiles
+  __host__ __device__ uint32_t tiles() const {
+    const int64_t first = (int64_t)len_k - len_q + (1 << per_log2);           // keys that the first task sees
+    const int least = !causal ? most() : first <= 0 ? 0 : first >= len_k ? most() : (int)((first + kPrTile - 1) / kPrTile);
+    return (uint32_t)(((int64_t)places * (most() + least) + 1) / 2);
+  }
+  __host__ __device__ int split(int L) const {
+    if (most() <= L || places <= 0) return 0;
+    const int64_t seen = (int64_t)L * kPrTile - ((int64_t)len_k - len_q);     // rows from the first on whose keys are L tiles or fewer
+    const int64_t from = !causal || seen <= 0 ? 0 : seen >> per_log2;
+    return from < places ? places - (int)from : 1;
+  }
+  __host__ __device__ int parts(int L) const {
+    const int p = (most() + L - 1) / L;
+    return p < 1 ? 1 : p > kPrParts ? kPrParts : p;
+  }
+  __host__ __device__ static int first_length(uint32_t all, int sms) {
+    const int share = (int)fminf((float)all * (1.25f / (float)sms), 1e9f) + 1;       // (a division of 64 bits would take longer than the search)
+    return share > kPrPartTiles ? share : kPrPartTiles;
+  }
+};
+
+// Where the tasks of up to 128 sequences begin and how many they are: lane l knows it of sequences l, l + 32, ...  Up to 32 are
+// taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short; more as they come.
+struct TaskOrder { int first[kPrHeld], count[kPrHeld], q0[kPrHeld], len_q[kPrHeld], k0[kPrHeld], len_k[kPrHeld], split, parts, slot; };
 //
-// Few query rows and many keys leave SMs idle: the keys of up to 32 sequences are then split, so that the tasks are at most as many as
-// the SMs (and as the workspace holds sums of).  With N tasks of t_i tiles, parts of L tiles are ceil(t_i / L) <= t_i / L + 1 tasks each,
-// which are at most C together if L >= sum t_i / (C - N).  (32 heads of 128 and 8 of keys: 64 queries behind 4 000 keys 62 -> 28 us, 256
-// behind 30 000 409 -> 161; 16 behind 100 000, 8 heads: 1 197 -> 76.  Fewer parts for the sake of the join, at most the
-// square root of the tiles: 30 us, 161, 81; parts of two tiles instead of four at the least: the same.)
+// Few query rows and many keys leave SMs idle: tasks of up to 32 sequences, where there are not more than SMs, are then split (Splitting).
 template <bool SPLIT>
 __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane) {
   TaskOrder o;
   int before = 0;
+  o.split = o.slot = 0;
   o.parts = 1;
-  o.slot = 0;
 #pragma unroll
   for (int i = 0; i < kPrHeld; ++i) {
     o.first[i] = o.count[i] = o.q0[i] = o.len_q[i] = o.k0[i] = o.len_k[i] = 0;
@@ -227,16 +253,19 @@ __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane)
     }
     if (P.n_seqs <= 32) {
       if constexpr (SPLIT) {
-        const uint32_t n = __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0]), most = (uint32_t)(P.split / P.units);
-        if (n < most) {                                      // (fewer than the SMs, and below 2^24 tiles each: no overflow)
-          const uint32_t tiles = (uint32_t)(max(keys, 0) + kPrTile - 1) / kPrTile;
-          const uint32_t all = __reduce_add_sync(0xffffffffu, (uint32_t)o.count[0] * tiles);
-          const uint32_t least = max((uint32_t)kPrPartTiles, (all + (most - n) - 1) / (most - n));
-          if (tiles > least) o.parts = (int)min((tiles + least - 1) / least, (uint32_t)kPrParts);
-          o.count[0] *= o.parts;
-          o.slot = o.parts > 1 ? o.count[0] : 0;
-          int v = o.slot;
-  #pragma unroll
+        const int places = o.count[0];
+        const uint32_t n = __reduce_add_sync(0xffffffffu, (uint32_t)places) * P.units;
+        if (n <= (uint32_t)P.sms) {                          // (and each below 2^24 tiles: no overflow)
+          Splitting s = {max(keys, 0), o.len_q[0], places, 8 - P.pack_log2, P.causal};
+          const uint32_t all = __reduce_add_sync(0xffffffffu, s.tiles()) * P.units;
+          int least = Splitting::first_length(all, P.sms);
+          while (__reduce_add_sync(0xffffffffu, (uint32_t)(s.split(least) * s.parts(least))) * P.units > (uint32_t)P.split) least += max(1, least / 8);
+          o.split = s.split(least);
+          o.parts = s.parts(least);
+          o.count[0] += o.split * (o.parts - 1);
+          int v = o.split * o.parts;
+          o.slot = v;
+#pragma unroll
           for (int k = 1; k < 32; k <<= 1) {
             const int u = __shfl_up_sync(0xffffffffu, v, k);
             if (lane >= k) v += u;
@@ -279,14 +308,22 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
       if (mine) {
         const int l = __ffs(mine) - 1;
         lo = l + 32 * i;
-        place = __shfl_sync(0xffffffffu, order.first[i] + order.count[i], l) - 1 - turn;      // last rows first
+        const int at = turn - __shfl_sync(0xffffffffu, order.first[i], l);
+        place = __shfl_sync(0xffffffffu, order.count[i], l) - 1 - at;      // last rows first
         ti.row0 = __shfl_sync(0xffffffffu, order.q0[i], l);
         ti.len_q = __shfl_sync(0xffffffffu, order.len_q[i], l);
         ti.key0 = __shfl_sync(0xffffffffu, order.k0[i], l);
         ti.len_k = __shfl_sync(0xffffffffu, order.len_k[i], l);
         if (SPLIT && i == 0) {
-          parts = __shfl_sync(0xffffffffu, order.parts, l);
-          slot = __shfl_sync(0xffffffffu, order.slot, l);
+          const int split = __shfl_sync(0xffffffffu, order.split, l), p = __shfl_sync(0xffffffffu, order.parts, l);
+          if (at < split * p) {
+            const int k = at / p;
+            parts = p;
+            ti.part = at - k * p;
+            slot = __shfl_sync(0xffffffffu, order.slot, l) + k * p;
+            place += at - k;                                 // the k-th from the last
+            place -= split * (p - 1);
+          }
         }
       }
     }
@@ -312,12 +349,7 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
       return false;
     }
   }
-  if (SPLIT && parts > 1) {
-    const int whole = place / parts;
-    ti.part = place - whole * parts;
-    place = whole;
-    ti.slot = (slot + place * parts) * P.units + unit * parts;
-  }
+  if (SPLIT && parts > 1) ti.slot = slot * P.units + unit * parts;
   if (place < 0 || place >= (ti.len_q + per - 1) >> per_log2) return false;
   ti.tok0 = place * per;
   ti.kv_head = unit / P.packs;
@@ -1008,18 +1040,25 @@ static int launch_prompt(cudaStream_t st, const void* Q, int ld_q, const void* K
   const int64_t tasks = (int64_t)P.M_q / (2 * kPrTile >> P.pack_log2) + P.n_seqs;
   if (tasks * P.units > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   P.n_tasks = (int)tasks;
-  // Keys are split on the device, which knows the lengths; whether it may, and the join with it, follows from the sizes, as if all sequences were
+  // Keys are split on the device, which knows the lengths; whether they are, and the join with it, follows from the sizes, as if all sequences were
   // equally long.  The join takes 4 to 7 us, as long as a task with four tiles: 100 queries behind 500 keys, 16 us, took 23 with it.
   P.split = 0;
+  P.sms = device_sm_count();
   if (P.n_seqs <= 32) {
-    const int per = 2 * kPrTile >> P.pack_log2, most = std::min(device_sm_count(), most_parts<HD>());
-    const int64_t n = ((int64_t)P.M_q + (int64_t)P.n_seqs * (per - 1)) / per * P.units, tiles = P.M_k / ((int64_t)P.n_seqs * kPrTile);
-    if (n < most && tiles >= std::max<int64_t>(kPrPartTiles, (n * tiles + (most - n) - 1) / (most - n)) + kPrSplitGain) P.split = most;
+    const int per_log2 = 8 - P.pack_log2, len_q = (P.M_q + P.n_seqs - 1) / P.n_seqs, len_k = P.M_k / P.n_seqs;
+    const Splitting s = {len_k, len_q, (len_q + (1 << per_log2) - 1) >> per_log2, per_log2, P.causal};
+    const int64_t n = (int64_t)s.places * P.n_seqs * P.units;
+    if (n <= P.sms) {
+      int L = Splitting::first_length((uint32_t)std::min<int64_t>((int64_t)s.tiles() * P.n_seqs * P.units, UINT32_MAX), P.sms);
+      while ((int64_t)s.split(L) * s.parts(L) * P.n_seqs * P.units > most_parts<HD>()) L += std::max(1, L / 8);
+      if (s.most() >= std::max(L, (s.most() + kPrParts - 1) / kPrParts) + kPrSplitGain) P.split = most_parts<HD>();
+    }
   }
   if (!P.split) return launch_tasks<HD, false>(st, (unsigned)(tasks * P.units), tmQ, tmK, tmV, P);
-  const int got = launch_tasks<HD, true>(st, (unsigned)std::max<int64_t>(tasks * P.units, P.split), tmQ, tmK, tmV, P);
+  const unsigned blocks = (unsigned)(tasks * P.units + P.split);
+  const int got = launch_tasks<HD, true>(st, blocks, tmQ, tmK, tmV, P);
   if (got != FPT_OK) return got;
-  if (launch_kernel(prompt_join_kernel<HD>, dim3((unsigned)P.split), dim3(kPrJoinThreads), 0, st, true, P) != cudaSuccess) return FPT_ERR_CUDA;
+  if (launch_kernel(prompt_join_kernel<HD>, dim3(blocks), dim3(kPrJoinThreads), 0, st, true, P) != cudaSuccess) return FPT_ERR_CUDA;
   return FPT_OK;
 }
 

@@ -878,3 +878,18 @@ PADDED = [
 @pytest.mark.parametrize("hd,n_q,n_kv,len_q,len_k,causal", PADDED)
 def test_prompt_heads_that_fill_no_tile(hd, n_q, n_kv, len_q, len_k, causal):
     test_prompt(hd, n_q, n_kv, len_q, len_k, causal)
+
+
+UNEVEN = [
+    # hd, n_q, n_kv, len_q, len_k (None: the same), causal: only the tasks with many keys are split
+    (64, 2, 2, [3000], None, True),
+    (128, 5, 1, [2900, 10], None, True),
+    (128, 4, 2, [900, 100, 700], [900, 2500, 1400], True),
+    (64, 8, 2, [64, 1, 300], [100, 6000, 3000], False),
+    (128, 16, 2, [400], [1500], True),
+]
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,len_q,len_k,causal", UNEVEN)
+def test_prompt_tasks_of_uneven_length(hd, n_q, n_kv, len_q, len_k, causal):
+    test_prompt_keys_in_parts(hd, n_q, n_kv, len_q, len_k, causal)
