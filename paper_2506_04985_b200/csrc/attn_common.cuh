@@ -2,6 +2,7 @@
 // checks of a paged cache.
 #pragma once
 
+#include "attn_rules.h"
 #include "fpt_internal.cuh"
 
 namespace fpt {
@@ -67,26 +68,37 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatil
 // What a page's codes are multiplied with before rounding.
 __device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435e-38f ? __fdiv_rn(1.0f, s) : 0.0f; }
 
-// A launch over the pages (or blocks of `block` rows) that packed sequences touch, without their lengths on the host:
-// sequence s, rows cu[s] .. cu[s+1]-1, is given floor(cu[s+1] / block) - floor(cu[s] / block) + 2 tasks, which
-// is at least the number of blocks that its rows can touch, and task `id` belongs to the s whose tasks it is among.  All sequences are looked at
-// side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the look: one round of
-// loads, where a binary search would wait for one load after the other.  block 0: a task for each row, place 0.
+// The task of this CTA in a launch over the pages (or blocks of rows) that packed sequences touch (attn_rules.h).  All sequences are
+// looked at side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the look: one round of
+// loads, where a binary search would wait for one load after the other.  Offsets that do not ascend can give one task to several
+// sequences, each with rows below M: the lowest has it, and its thread alone says what it found, so that no first row of one meets the
+// rows of another.
 struct FoundTask { int seq, place, row0, rows, extra; };
 __device__ __forceinline__ FoundTask find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int M, int block,
                                                int id, FoundTask* found /* shared */, uint32_t* status) {
-  if (threadIdx.x == 0) found->seq = -1;
+  if (threadIdx.x == 0) found->seq = INT32_MAX;
   __syncthreads();
+  FoundTask mine = {INT32_MAX, 0, 0, 0, 0};
   for (int s = threadIdx.x; s < n_seqs; s += blockDim.x) {
     const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1), e = extra ? __ldg(extra + s) : 0;
-    if (lo < 0 || hi < lo || hi > M) {
+    if (!rows_fit(lo, hi, M)) {
       if (blockIdx.x == 0) record_bad_index(status, kBadOffset);
-    } else if (block == 0) {
-      if (lo <= id && id < hi) *found = FoundTask{s, 0, lo, hi - lo, e};
     } else {
-      const int a = lo / block + 2 * s;
-      if (a <= id && id < hi / block + 2 * s + 2) *found = FoundTask{s, id - a, lo, hi - lo, e};
+      const int place = place_of_task(lo, hi, s, block, id);
+      if (place >= 0 && mine.seq == INT32_MAX) {
+        mine = FoundTask{s, place, lo, hi - lo, e};
+        atomicMin(&found->seq, s);
+      }
     }
+  }
+  __syncthreads();
+  const int winner = found->seq;
+  if (winner == INT32_MAX) return FoundTask{-1, 0, 0, 0, 0};
+  if (mine.seq == winner) {                          // (one thread)
+    found->place = mine.place;
+    found->row0 = mine.row0;
+    found->rows = mine.rows;
+    found->extra = mine.extra;
   }
   __syncthreads();
   return *found;

@@ -422,7 +422,7 @@ extern "C" int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int
   cudaStream_t st = (cudaStream_t)stream;
   // The pages that the rows may touch, numbered without their lengths; few rows a sequence: a task for each row, of which the first in a page
   // works (64 sequences of one token, 16 CTAs a task: 7.6 -> 5.7 us).
-  const int64_t by_page = (int64_t)M / P.page + 2 * (int64_t)n_seqs;
+  const int64_t by_page = block_tasks(M, n_seqs, P.page);
   P.by_row = cu_new && M < by_page;
   const int64_t tasks = !cu_new ? n_seqs : P.by_row ? M : by_page;
   if (tasks > INT32_MAX) return FPT_ERR_UNSUPPORTED;
@@ -457,7 +457,7 @@ extern "C" int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int3
   P.status = reinterpret_cast<uint32_t*>(workspace);
   P.M = M; P.ld = ld; P.n_kv = cache->n_kv; P.n_seqs = n_seqs; P.n_pages = cache->n_pages; P.page = cache->page;
   P.max_pages = cache->max_pages;
-  const int64_t tasks = (int64_t)M / P.page + 2 * (int64_t)n_seqs;
+  const int64_t tasks = block_tasks(M, n_seqs, P.page);
   if (tasks > INT32_MAX) return FPT_ERR_UNSUPPORTED;
   P.heads = 8192 / (cache->page * cache->head_dim);
   if (P.heads < 1) P.heads = 1;

@@ -1,0 +1,37 @@
+"""The attention calls at the edges of what they allow: batches without a row or a key, offsets that do not ascend, codes of errors beside
+one another, what a program does between calls."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as OA
+from paper_2506_04985_b200 import binding as B
+from helpers import DEV, bf16_host, guarded_empty, host
+from test_gpu_attn import bf16, check_decode, check_prompt, decode_case, i32, offsets, paged, prompt_case, table, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n,rows", [(3, 1000), (41, 1000), (300, 2000), (300, 400)])
+def test_offsets_that_do_not_ascend_stay_inside_the_buffers(n, rows):
+    """Sequences that are fine by themselves claim the same tasks, from one warp and from several; outputs end with their guard bands, rows of
+    the cache's pages that no sequence has stay as they were."""
+    rng = np.random.default_rng(n)
+    hd, page, n_q, n_kv = 64, 16, 2, 1
+    cu = [0, rows] + [5 + i * (rows - 90) // n for i in range(n - 2)] + [rows]
+    cache, pages, codes, scales = paged(rng, [max(b - a, 0) + page for a, b in zip(cu, cu[1:])], page, n_kv, hd)
+    x, tab = bf16(rng, rows, (n_q + 2 * n_kv) * hd).to(DEV), torch.from_numpy(table(rows + 64, hd)).to(DEV)
+    for _ in range(3):
+        ws = workspace()
+        ctx = i32([int(c) for c in rng.integers(0, page, n)])
+        Q, K = guarded_empty((rows, n_q * hd), torch.bfloat16), guarded_empty((rows, n_kv * hd), torch.bfloat16)
+        B.fpt_rope_append(x, n_q, cache, tab, ctx, cu_new=i32(cu), Q=Q, K=K, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX
+        ws = workspace()
+        K, V = guarded_empty((rows, n_kv * hd), torch.bfloat16), guarded_empty((rows, n_kv * hd), torch.bfloat16)
+        B.fpt_kv_gather(cache, i32(cu), rows, first=ctx, K=K, V=V, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX
+    free = sorted(set(range(cache.k.shape[0])) - {int(p) for p in pages.ravel() if p >= 0})
+    assert len(free) == 2 and np.array_equal(host(cache.k)[free], codes[0][free]) and np.array_equal(host(cache.v_scale)[free], scales[1][free])
