@@ -368,8 +368,8 @@ int fpt_decoder_attn_out(void* stream, const void* A, int M, int k_o,
  * or 8-bit values is 16-byte aligned, every other one naturally.
  *
  * Lengths, offsets, positions and page numbers lie on the device and are not known to the host: one out of range
- * never leads outside a buffer; it is recorded in the status word (fpt_check_status returns FPT_ERR_INDEX until
- * fpt_reset_status), and the results of the sequences it concerns are unspecified.
+ * never leads outside a buffer; it is recorded beside the status word (fpt_check_status returns FPT_ERR_INDEX until
+ * fpt_reset_status, FPT_ERR_TIMEOUT where a wait gave up too), and the results of the sequences it concerns are unspecified.
  *
  * The four calls take a workspace of fpt_workspace_bytes(FPT_OP_ATTN, 1, 1, 1) bytes (any sizes), cleared once by
  * fpt_reset_status.  It may be the one that the linears use if it is large enough, and as there, calls that may run
@@ -488,7 +488,7 @@ size_t fpt_workspace_bytes(int op, int M, int N, int K);
  * after allocating it, and again after a call that ended in FPT_ERR_TIMEOUT. */
 int fpt_reset_status(void* stream, void* workspace);
 
-/* Synchronises `stream`, reads the status word at the start of `workspace` and returns
+/* Synchronises `stream`, reads the status words at the start of `workspace` and returns
  * FPT_OK, FPT_ERR_TIMEOUT (a bounded device-side wait expired; the kernel released its
  * resources and returned, outputs are invalid), FPT_ERR_INDEX (the attention calls) or FPT_ERR_CUDA. */
 int fpt_check_status(void* stream, void* workspace);

@@ -152,11 +152,12 @@ extern "C" int fpt_reset_status(void* stream, void* workspace) {
 
 extern "C" int fpt_check_status(void* stream, void* workspace) {
   if (!workspace) return FPT_ERR_BAD_ARG;
-  uint32_t word = 0;
-  if (cudaMemcpyAsync(&word, workspace, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess)
+  uint32_t words[kIndexWord + 1] = {};
+  if (cudaMemcpyAsync(words, workspace, sizeof words, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess)
     return FPT_ERR_CUDA;
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return FPT_ERR_CUDA;
-  return word == 0 ? FPT_OK : (word & ~0xFFu) == kStatusIndexBase ? FPT_ERR_INDEX : FPT_ERR_TIMEOUT;
+  if (words[0]) return FPT_ERR_TIMEOUT;
+  return (words[kIndexWord] & ~0xFFu) == kStatusIndexBase ? FPT_ERR_INDEX : FPT_OK;
 }
 
 // fpt_w4a4_gemm; `early`: see GemmParams::early_weights, `wide`: the codes are widened, [M, K] bytes (only the composed

@@ -7,12 +7,15 @@
 
 namespace fpt {
 
-constexpr uint32_t kStatusIndexBase = 0x7200u;       // status word: a page, position, length or offset was out of range
+// A page, position, length or offset was out of range: a word of its own behind the status word, so that a wait that gave up, in
+// whatever call on the workspace, is never covered up.
+constexpr int kIndexWord = 1;
+constexpr uint32_t kStatusIndexBase = 0x7200u;
 enum : uint32_t { kBadPage = 1, kBadPosition = 2, kBadLength = 3, kBadOffset = 4 };
+static_assert(kIndexWord < kCounterWord0, "a counter's place");
 
-// First one wins; a time-out is never covered up.
-__device__ __forceinline__ void record_bad_index(uint32_t* status, uint32_t what) {
-  atomicCAS(status, 0u, kStatusIndexBase | what);
+__device__ __forceinline__ void record_bad_index(uint32_t* status, uint32_t what) {      // the first one stays
+  atomicCAS(status + kIndexWord, 0u, kStatusIndexBase | what);
 }
 
 // The i-th of four two's complement bytes whose sign bits the caller has flipped, as a float32: 2^23 + (code + 128) is

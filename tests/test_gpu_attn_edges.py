@@ -35,3 +35,23 @@ def test_offsets_that_do_not_ascend_stay_inside_the_buffers(n, rows):
         assert B.fpt_check_status(ws) == B.ERR_INDEX
     free = sorted(set(range(cache.k.shape[0])) - {int(p) for p in pages.ravel() if p >= 0})
     assert len(free) == 2 and np.array_equal(host(cache.k)[free], codes[0][free]) and np.array_equal(host(cache.v_scale)[free], scales[1][free])
+
+
+def test_an_index_out_of_range_covers_no_wait_that_gave_up():
+    """Both kinds of error on one workspace, in either order: the one that spoils every output is the one that is reported."""
+    rng = np.random.default_rng(2)
+    cache, _, _, _, q = decode_case(rng, 64, 16, 2, 1, [20])
+    q, too_long = q.to(DEV), i32([1 << 20])
+    for order in (0, 1):
+        ws = workspace()
+        for what in ("index", "wait") if order == 0 else ("wait", "index"):
+            if what == "index":
+                B.fpt_attn_decode(q, cache, too_long, ws=ws)
+                assert B.fpt_check_status(ws) == (B.ERR_INDEX if order == 0 else B.ERR_TIMEOUT)
+            else:
+                B.fpt_selftest_wait_timeout(ws, limit_us=2000)
+                assert B.fpt_check_status(ws) == B.ERR_TIMEOUT
+        assert B.lib().fpt_reset_status(B._stream(), B._ptr(ws)) == B.OK
+        assert B.fpt_check_status(ws) == B.OK
+        B.fpt_attn_decode(q, cache, too_long, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX
