@@ -50,24 +50,47 @@ class _KVCacheStruct(ctypes.Structure):
 
 class KVCache:
     """A paged 8-bit cache (see `fpt_kv_cache`): codes int8 [n_pages, n_kv, page, head_dim], scales f32 [n_pages, n_kv],
-    page table int32 [n_seqs, max_pages], all contiguous on one device."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "n_seqs", "n_kv", "head_dim", "dev", "ref")
+    page table int32 [n_seqs, max_pages], all contiguous on one device.  Calls take the tensors as they are then: a longer page
+    table, say, may be put in the place of `pages` between two of them."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "_bare")
 
     def __init__(self, k, v, k_scale, v_scale, pages):
-        described = (_calls or _native()).describe_cache(k, v, k_scale, v_scale, pages)
-        if described is None:
+        self.k, self.v, self.k_scale, self.v_scale, self.pages, self._bare = k, v, k_scale, v_scale, pages, None
+        if self.ref is None:
             raise ValueError("KVCache: contiguous int8 codes, float32 scales and an int32 page table on one device are wanted")
-        self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
-        self.ref, self.n_seqs, self.n_kv, self.head_dim, self.dev = described         # ref: the struct's bytes
 
     @classmethod
     def heads(cls, n_kv, head_dim):
         """Stands for no storage: fpt_rope_append then only rotates."""
         c = cls.__new__(cls)
         c.k = c.v = c.k_scale = c.v_scale = c.pages = None
-        c.n_seqs, c.n_kv, c.head_dim, c.dev = 0, n_kv, head_dim, -1
-        c.ref = bytes(_KVCacheStruct(None, None, None, None, None, 0, n_kv, 0, head_dim, 0))
+        c._bare = (n_kv, head_dim)
+        c.ref                                               # (raises where these are no numbers)
         return c
+
+    @property
+    def ref(self):
+        """The bytes of the `fpt_kv_cache` that a call is given; None: the tensors are no cache."""
+        if self._bare is not None:
+            return bytes(_KVCacheStruct(None, None, None, None, None, 0, self._bare[0], 0, self._bare[1], 0))
+        return (_calls or _native()).describe_cache(self.k, self.v, self.k_scale, self.v_scale, self.pages)
+
+    @property
+    def n_seqs(self):
+        return self.pages.shape[0] if self._bare is None else 0
+
+    @property
+    def n_kv(self):
+        return self.k.shape[1] if self._bare is None else self._bare[0]
+
+    @property
+    def head_dim(self):
+        return self.k.shape[3] if self._bare is None else self._bare[1]
+
+    @property
+    def dev(self):
+        """Index of its GPU, -1: none."""
+        return self.k.get_device() if self._bare is None else -1
 
 
 class FptError(RuntimeError):
@@ -387,21 +410,22 @@ def fpt_rope_append(QKV, n_q, cache, rope, ctx, cu_new=None, layout=ROPE_HALF, w
     Keys and values go to the cache (KVCache.heads(n_kv, head_dim): nowhere)."""
     if ws is None:
         ws = _scratch(QKV, "fpt_rope_append")
-    return (_calls or _native()).rope_append(QKV, n_q, cache.ref, cache.n_seqs, cache.dev, rope, ctx, cu_new, layout, want_k, Q, K, ws)
+    return (_calls or _native()).rope_append(QKV, n_q, cache.k, cache.v, cache.k_scale, cache.v_scale, cache.pages, cache._bare, rope, ctx, cu_new,
+                                             layout, want_k, Q, K, ws)
 
 
 def fpt_kv_gather(cache, cu_out, M, first=None, K=None, V=None, ws=None):
     """Cached tokens first[s] ... of every sequence in bf16 -> (K, V) [M, n_kv head_dim], packed by cu_out int32 [n_seqs + 1]."""
     if ws is None:
         ws = _scratch(cu_out, "fpt_kv_gather")
-    return (_calls or _native()).kv_gather(cache.ref, cache.n_seqs, cache.dev, cu_out, M, first, K, V, ws)
+    return (_calls or _native()).kv_gather(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.pages, cu_out, M, first, K, V, ws)
 
 
 def fpt_attn_decode(Q, cache, kv_len, scale=None, want_lse=False, O=None, ws=None):
     """Q [n_seqs, n_q head_dim] bf16, kv_len int32 [n_seqs] -> (O like Q, lse f32 [n_seqs, n_q] or None)."""
     if ws is None:
         ws = _scratch(Q, "fpt_attn_decode")
-    return (_calls or _native()).attn_decode(Q, cache.ref, cache.n_seqs, cache.dev, kv_len, scale, want_lse, O, ws)
+    return (_calls or _native()).attn_decode(Q, cache.k, cache.v, cache.k_scale, cache.v_scale, cache.pages, kv_len, scale, want_lse, O, ws)
 
 
 def fpt_attn_prompt(Q, K, V, n_q, n_kv, cu_q, cu_k=None, causal=True, scale=None, want_lse=False, O=None, ws=None):

@@ -136,10 +136,43 @@ PyObject* pair(Held& a, Held& b) {
   return r;
 }
 
-const fpt_kv_cache* cache_of(PyObject* ref, const char* where) {
-  if (!PyBytes_Check(ref) || PyBytes_GET_SIZE(ref) != (Py_ssize_t)sizeof(fpt_kv_cache)) refuse(where, FPT_ERR_BAD_ARG);
-  return reinterpret_cast<const fpt_kv_cache*>(PyBytes_AS_STRING(ref));
-}
+// The five tensors of a cache, as they are at this call: a caller may put another page table or other storage in their places.
+struct Cache : fpt_kv_cache {
+  int64_t n_seqs;
+  int dev;                        // -1: not on a GPU
+
+  // k, v, k_scale, v_scale, pages: whether they are a cache
+  bool read(PyObject* const* a) {
+    for (int i = 0; i < 5; ++i)
+      if (!THPVariable_Check(a[i])) return false;
+    const at::Tensor &tk = THPVariable_Unpack(a[0]), &tv = THPVariable_Unpack(a[1]), &ks = THPVariable_Unpack(a[2]), &vs = THPVariable_Unpack(a[3]),
+                     &table = THPVariable_Unpack(a[4]);
+    if (tk.dim() != 4 || table.dim() != 2 || tk.scalar_type() != at::kChar || tv.scalar_type() != at::kChar || ks.scalar_type() != at::kFloat ||
+        vs.scalar_type() != at::kFloat || table.scalar_type() != at::kInt || tv.sizes() != tk.sizes() || ks.sizes() != tk.sizes().slice(0, 2) ||
+        vs.sizes() != ks.sizes() || !tk.is_contiguous() || !tv.is_contiguous() || !ks.is_contiguous() || !vs.is_contiguous() ||
+        !table.is_contiguous())
+      return false;
+    for (const at::Tensor* t : {&tv, &ks, &vs, &table})
+      if (t->device() != tk.device()) return false;
+    for (int i = 0; i < 4; ++i)
+      if (tk.size(i) > INT_MAX) return false;
+    if (table.size(0) > INT_MAX || table.size(1) > INT_MAX) return false;
+    static_cast<fpt_kv_cache&>(*this) = fpt_kv_cache{};
+    k = static_cast<int8_t*>(tk.data_ptr());
+    v = static_cast<int8_t*>(tv.data_ptr());
+    k_scale = static_cast<float*>(ks.data_ptr());
+    v_scale = static_cast<float*>(vs.data_ptr());
+    pages = static_cast<const int32_t*>(table.data_ptr());
+    n_pages = (int)tk.size(0);
+    n_kv = (int)tk.size(1);
+    page = (int)tk.size(2);
+    head_dim = (int)tk.size(3);
+    max_pages = (int)table.size(1);
+    n_seqs = table.size(0);
+    dev = tk.is_cuda() ? (int)tk.get_device() : -1;
+    return true;
+  }
+};
 
 template <class F>
 PyObject* guarded(F f) {
@@ -175,62 +208,45 @@ PyObject* set_allocator(PyObject*, PyObject* fn) {
   Py_RETURN_NONE;
 }
 
-// (k, v, k_scale, v_scale, pages) -> (fpt_kv_cache as bytes, n_seqs, n_kv, head_dim, device index), or None if they are no cache
+// (k, v, k_scale, v_scale, pages) -> fpt_kv_cache as bytes, or None if they are no cache
 PyObject* describe_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arguments(n, 5)) return nullptr;
   return guarded([&]() -> PyObject* {
-    for (int i = 0; i < 5; ++i)
-      if (!THPVariable_Check(a[i])) Py_RETURN_NONE;
-    const at::Tensor &k = THPVariable_Unpack(a[0]), &v = THPVariable_Unpack(a[1]), &ks = THPVariable_Unpack(a[2]), &vs = THPVariable_Unpack(a[3]),
-                     &pages = THPVariable_Unpack(a[4]);
-    if (k.dim() != 4 || pages.dim() != 2 || k.scalar_type() != at::kChar || v.scalar_type() != at::kChar || ks.scalar_type() != at::kFloat ||
-        vs.scalar_type() != at::kFloat || pages.scalar_type() != at::kInt || v.sizes() != k.sizes() || ks.sizes() != k.sizes().slice(0, 2) ||
-        vs.sizes() != ks.sizes() || !k.is_contiguous() || !v.is_contiguous() || !ks.is_contiguous() || !vs.is_contiguous() ||
-        !pages.is_contiguous())
-      Py_RETURN_NONE;
-    for (const at::Tensor* t : {&v, &ks, &vs, &pages})
-      if (t->device() != k.device()) Py_RETURN_NONE;
-    for (int i = 0; i < 4; ++i)
-      if (k.size(i) > INT_MAX) Py_RETURN_NONE;
-    if (pages.size(0) > INT_MAX || pages.size(1) > INT_MAX) Py_RETURN_NONE;
-    fpt_kv_cache c{};
-    c.k = static_cast<int8_t*>(k.data_ptr());
-    c.v = static_cast<int8_t*>(v.data_ptr());
-    c.k_scale = static_cast<float*>(ks.data_ptr());
-    c.v_scale = static_cast<float*>(vs.data_ptr());
-    c.pages = static_cast<const int32_t*>(pages.data_ptr());
-    c.n_pages = (int)k.size(0);
-    c.n_kv = (int)k.size(1);
-    c.page = (int)k.size(2);
-    c.head_dim = (int)k.size(3);
-    c.max_pages = (int)pages.size(1);
-    return Py_BuildValue("(y#iiii)", reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof c, (int)pages.size(0), c.n_kv, c.head_dim,
-                         k.is_cuda() ? (int)k.get_device() : -1);
+    Cache c;
+    if (!c.read(a)) Py_RETURN_NONE;
+    return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(static_cast<fpt_kv_cache*>(&c)), (Py_ssize_t)sizeof(fpt_kv_cache));
   });
 }
 
-// QKV, n_q, cache struct, its n_seqs, its device, rope, ctx, cu_new, layout, want_k, Q, K, workspace
+// QKV, n_q, the cache's tensors, None or (n_kv, head_dim) of a cache without storage, rope, ctx, cu_new, layout, want_k, Q, K, workspace
 PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 13)) return nullptr;
+  if (!arguments(n, 16)) return nullptr;
   return guarded([&]() -> PyObject* {
     const char* where = "fpt_rope_append";
     Call c(where, Call::tensor(a[0], where));
     const at::Tensor& x = c.rows(a[0]);
     const int n_q = whole32(a[1], where);
-    const fpt_kv_cache* cache = cache_of(a[2], where);
-    const at::Tensor &rope = c.on(a[5], at::kFloat), &ctx = c.on(a[6], at::kInt), &ws = c.scratch(a[12]);
-    const int64_t M = x.size(0), hd = cache->head_dim, n_kv = cache->n_kv;
+    Cache cache{};
+    if (a[7] == Py_None) {
+      c.need(cache.read(a + 2) && cache.k && cache.dev == c.dev);
+    } else {
+      c.need(PyTuple_Check(a[7]) && PyTuple_GET_SIZE(a[7]) == 2);
+      cache.n_kv = whole32(PyTuple_GET_ITEM(a[7], 0), where);
+      cache.head_dim = whole32(PyTuple_GET_ITEM(a[7], 1), where);
+    }
+    const at::Tensor &rope = c.on(a[8], at::kFloat), &ctx = c.on(a[9], at::kInt), &ws = c.scratch(a[15]);
+    const int64_t M = x.size(0), hd = cache.head_dim, n_kv = cache.n_kv;
     c.need(rope.dim() == 3 && rope.size(2) == 2 && rope.is_contiguous() && rope.size(0) <= INT_MAX && rope.size(1) <= 1024 && ctx.dim() == 1);
     const int64_t n_seqs = ctx.size(0);
     c.need(n_q >= 0 && n_kv >= 0 && hd >= 0 && n_seqs <= INT_MAX && x.size(1) >= (n_q + 2 * n_kv) * hd);
-    c.need(!cache->k || (whole(a[3]) >= n_seqs && whole(a[4]) == c.dev));
-    Held q{c.result(a[10], false, M, n_q * hd)}, k{a[11] != Py_None || truth(a[9]) ? c.result(a[11], false, M, n_kv * hd) : nullptr};
-    const int32_t *cu = a[7] == Py_None ? nullptr : c.indices(a[7], n_seqs + 1), *have = c.indices(a[6], n_seqs);
-    const int layout = whole32(a[8], where);
+    c.need(!cache.k || cache.n_seqs >= n_seqs);
+    Held q{c.result(a[13], false, M, n_q * hd)}, k{a[14] != Py_None || truth(a[12]) ? c.result(a[14], false, M, n_kv * hd) : nullptr};
+    const int32_t *cu = a[10] == Py_None ? nullptr : c.indices(a[10], n_seqs + 1), *have = c.indices(a[9], n_seqs);
+    const int layout = whole32(a[11], where);
     int code;
     Py_BEGIN_ALLOW_THREADS
     code = c_rope_append(c.stream, x.data_ptr(), (int)M, Call::ld(x), n_q, static_cast<const float*>(rope.data_ptr()), (int)rope.size(0),
-                         2 * (int)rope.size(1), layout, cu, have, (int)n_seqs, cache, q.t().data_ptr(), Call::ld(q.t()),
+                         2 * (int)rope.size(1), layout, cu, have, (int)n_seqs, &cache, q.t().data_ptr(), Call::ld(q.t()),
                          k.o ? k.t().data_ptr() : nullptr, k.o ? Call::ld(k.t()) : 0, ws.data_ptr(), (size_t)ws.numel());
     Py_END_ALLOW_THREADS
     c.done(code);
@@ -238,25 +254,26 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// cache struct, its n_seqs, its device, cu_out, M, first, K, V, workspace
+// the cache's tensors, cu_out, M, first, K, V, workspace
 PyObject* kv_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 9)) return nullptr;
+  if (!arguments(n, 11)) return nullptr;
   return guarded([&]() -> PyObject* {
     const char* where = "fpt_kv_gather";
-    const at::Tensor& cu = Call::tensor(a[3], where);
+    const at::Tensor& cu = Call::tensor(a[5], where);
     Call c(where, cu);
-    const fpt_kv_cache* cache = cache_of(a[0], where);
+    Cache cache;
+    c.need(cache.read(a) && cache.k && cache.dev == c.dev);
     c.need(cu.dim() == 1 && cu.size(0) >= 1 && cu.size(0) <= INT_MAX);
-    const int64_t n_seqs = cu.size(0) - 1, cols = (int64_t)cache->n_kv * cache->head_dim;
-    const int M = whole32(a[4], where);
-    c.need(cache->k && M >= 0 && whole(a[1]) >= n_seqs && whole(a[2]) == c.dev);
-    const int32_t *ends = c.indices(a[3], n_seqs + 1), *first = a[5] == Py_None ? nullptr : c.indices(a[5], n_seqs);
-    const at::Tensor& ws = c.scratch(a[8]);
-    Held k{c.result(a[6], false, M, cols)}, v{c.result(a[7], false, M, cols)};
+    const int64_t n_seqs = cu.size(0) - 1, cols = (int64_t)cache.n_kv * cache.head_dim;
+    const int M = whole32(a[6], where);
+    c.need(M >= 0 && cache.n_seqs >= n_seqs);
+    const int32_t *ends = c.indices(a[5], n_seqs + 1), *first = a[7] == Py_None ? nullptr : c.indices(a[7], n_seqs);
+    const at::Tensor& ws = c.scratch(a[10]);
+    Held k{c.result(a[8], false, M, cols)}, v{c.result(a[9], false, M, cols)};
     c.need(Call::ld(k.t()) == Call::ld(v.t()));
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = c_kv_gather(c.stream, cache, first, ends, (int)n_seqs, M, k.t().data_ptr(), v.t().data_ptr(), Call::ld(k.t()), ws.data_ptr(),
+    code = c_kv_gather(c.stream, &cache, first, ends, (int)n_seqs, M, k.t().data_ptr(), v.t().data_ptr(), Call::ld(k.t()), ws.data_ptr(),
                        (size_t)ws.numel());
     Py_END_ALLOW_THREADS
     c.done(code);
@@ -271,24 +288,25 @@ float scale_of(PyObject* o, int64_t head_dim) {
   return (float)v;
 }
 
-// Q, cache struct, its n_seqs, its device, kv_len, scale, want_lse, O, workspace
+// Q, the cache's tensors, kv_len, scale, want_lse, O, workspace
 PyObject* attn_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arguments(n, 9)) return nullptr;
+  if (!arguments(n, 11)) return nullptr;
   return guarded([&]() -> PyObject* {
     const char* where = "fpt_attn_decode";
     Call c(where, Call::tensor(a[0], where));
     const at::Tensor& q = c.rows(a[0]);
-    const fpt_kv_cache* cache = cache_of(a[1], where);
-    const int64_t n_seqs = q.size(0), hd = cache->head_dim;
-    c.need(cache->k && hd > 0 && q.size(1) % hd == 0 && whole(a[2]) >= n_seqs && whole(a[3]) == c.dev);
+    Cache cache;
+    c.need(cache.read(a + 1) && cache.k && cache.dev == c.dev);
+    const int64_t n_seqs = q.size(0), hd = cache.head_dim;
+    c.need(hd > 0 && q.size(1) % hd == 0 && cache.n_seqs >= n_seqs);
     const int n_q = (int)(q.size(1) / hd);
-    const int32_t* len = c.indices(a[4], n_seqs);
-    const at::Tensor& ws = c.scratch(a[8]);
-    const float scale = scale_of(a[5], hd);
-    Held o{c.result(a[7], false, n_seqs, q.size(1))}, lse{truth(a[6]) ? c.result(Py_None, true, n_seqs, n_q) : nullptr};
+    const int32_t* len = c.indices(a[6], n_seqs);
+    const at::Tensor& ws = c.scratch(a[10]);
+    const float scale = scale_of(a[7], hd);
+    Held o{c.result(a[9], false, n_seqs, q.size(1))}, lse{truth(a[8]) ? c.result(Py_None, true, n_seqs, n_q) : nullptr};
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = c_attn_decode(c.stream, q.data_ptr(), Call::ld(q), n_q, cache, len, (int)n_seqs, scale, o.t().data_ptr(), Call::ld(o.t()),
+    code = c_attn_decode(c.stream, q.data_ptr(), Call::ld(q), n_q, &cache, len, (int)n_seqs, scale, o.t().data_ptr(), Call::ld(o.t()),
                          lse.o ? static_cast<float*>(lse.t().data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel());
     Py_END_ALLOW_THREADS
     c.done(code);

@@ -55,3 +55,34 @@ def test_an_index_out_of_range_covers_no_wait_that_gave_up():
         assert B.fpt_check_status(ws) == B.OK
         B.fpt_attn_decode(q, cache, too_long, ws=ws)
         assert B.fpt_check_status(ws) == B.ERR_INDEX
+
+
+def test_a_page_table_that_grows_between_calls():
+    """A server's way: the table and the storage of a cache are replaced as contexts grow; the old ones' memory goes to others."""
+    rng = np.random.default_rng(3)
+    hd, page, n_q, n_kv = 64, 16, 4, 2
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, [60, 9])
+    q, ws = q.to(DEV), workspace()
+    whole, table_2 = pages.copy(), torch.from_numpy(pages[:1, :2].copy()).to(DEV)
+    cache.pages = table_2
+    o, _ = B.fpt_attn_decode(q[:1], cache, i32([30]), ws=ws)
+    check_decode(o, None, [30], pages, codes, scales, q.cpu(), n_q, hd, page, hd ** -0.5)
+    with pytest.raises(B.FptError):                        # a row that this table has not
+        B.fpt_attn_decode(q, cache, i32([30, 9]), ws=ws)
+    cache.pages = i32(whole.tolist())
+    del table_2
+    spoil = [torch.full((1, 2), 1 << 29, dtype=torch.int32, device=DEV) for _ in range(8)]
+    for name in ("k", "v", "k_scale", "v_scale"):
+        setattr(cache, name, getattr(cache, name).clone())
+    o, _ = B.fpt_attn_decode(q, cache, i32([60, 9]), ws=ws)
+    assert B.fpt_check_status(ws) == B.OK and len(spoil) == 8
+    check_decode(o, None, [60, 9], pages, codes, scales, q.cpu(), n_q, hd, page, hd ** -0.5)
+    x, tab = bf16(rng, 1, (n_q + 2 * n_kv) * hd).to(DEV), torch.from_numpy(table(70, hd)).to(DEV)
+    keep = cache.pages
+    for bad in (keep.long(), keep.cpu(), keep[:, ::2], None):
+        cache.pages = bad
+        for call in (lambda: B.fpt_attn_decode(q, cache, i32([60, 9])), lambda: B.fpt_kv_gather(cache, i32([0, 5]), 5),
+                     lambda: B.fpt_rope_append(x, n_q, cache, tab, i32([60]))):
+            with pytest.raises(B.FptError) as e:
+                call()
+            assert e.value.code == B.ERR_BAD_ARG
