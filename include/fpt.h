@@ -419,7 +419,7 @@ int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int n_q,
 
 /*
  * Cached tokens in 16 bits: row cu_out[s] + i of K_out and V_out [M, ld] (n_kv heads of head_dim) becomes
- * bf16(code * scale) of token first[s] + i (first NULL: 0).
+ * bf16(code * scale) of token first[s] + i (first NULL: 0).  M = 0, with K_out and V_out NULL: no sequence has rows.
  */
 int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int32_t* first, const int32_t* cu_out, int n_seqs,
                   int M, void* K_out, void* V_out, int ld, void* workspace, size_t workspace_bytes);
@@ -442,6 +442,7 @@ int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, const fpt_kv
  * causal = 1 only those with j <= i + (len_k - len_q), so that the last query sees the last key; a row that sees none gives O = 0, lse = -inf.
  *   Q [M_q, ld_q], K and V [M_k, ld_k], [M_k, ld_v], O [M_q, ld_o] bf16; lse [M_q, n_q] f32 or NULL
  *   cu_q, cu_k [n_seqs + 1]; cu_k NULL: cu_q.  Q, K and V may be places in one buffer; O overlaps none of them.
+ *   M_k = 0, with K and V NULL: no sequence has keys.
  * float32 scores and sums; the weights enter the second product in bf16, scaled so that a row's largest is at most 2^8: values below
  * 2^119 / len_k in magnitude overflow no sum.  Values of hidden keys, infinities and NaN among them, reach no result.
  * Where few query rows would leave SMs idle, keys are split over them by the sizes and the lengths of all sequences, and a

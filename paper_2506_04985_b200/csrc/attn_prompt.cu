@@ -1034,8 +1034,11 @@ static int launch_tasks(cudaStream_t st, unsigned blocks, const CUtensorMap& tmQ
 template <int HD>
 static int launch_prompt(cudaStream_t st, const void* Q, int ld_q, const void* K, int ld_k, const void* V, PromptParams P) {
   CUtensorMap tmQ, tmK, tmV;
-  if (!make_query_map(&tmQ, Q, HD, P.n_q, P.M_q, ld_q, 1 << P.pack_log2) || !make_rows_map(&tmK, K, P.n_kv * HD, P.M_k, ld_k) ||
-      !make_rows_map(&tmV, V, P.n_kv * HD, P.M_k, P.ld_v))
+  // Without keys nothing is fetched; a map has to have a row all the same.
+  const bool keys = P.M_k > 0;
+  if (!make_query_map(&tmQ, Q, HD, P.n_q, P.M_q, ld_q, 1 << P.pack_log2) ||
+      !make_rows_map(&tmK, keys ? K : Q, P.n_kv * HD, keys ? P.M_k : 1, keys ? ld_k : ld_q) ||
+      !make_rows_map(&tmV, keys ? V : Q, P.n_kv * HD, keys ? P.M_k : 1, keys ? P.ld_v : ld_q))
     return FPT_ERR_CUDA;
   const int64_t tasks = (int64_t)P.M_q / (2 * kPrTile >> P.pack_log2) + P.n_seqs;
   if (tasks * P.units > INT32_MAX) return FPT_ERR_UNSUPPORTED;
@@ -1070,7 +1073,8 @@ extern "C" int fpt_attn_prompt(void* stream, const void* Q, int ld_q, int M_q, c
                                int M_k, int n_q, int n_kv, int head_dim, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,
                                int causal, float scale, void* O, int ld_o, float* lse, void* workspace,
                                size_t workspace_bytes) {
-  if (!Q || !K || !V || !O || !cu_q || M_q <= 0 || M_k <= 0 || n_q <= 0 || n_kv <= 0 || n_seqs <= 0) return FPT_ERR_BAD_ARG;
+  if (!Q || !O || !cu_q || M_q <= 0 || M_k < 0 || !K != (M_k == 0) || !V != (M_k == 0) || n_q <= 0 || n_kv <= 0 || n_seqs <= 0)
+    return FPT_ERR_BAD_ARG;
   if (head_dim != 64 && head_dim != 128) return FPT_ERR_UNSUPPORTED;
   if (n_q % n_kv || n_q > 65535) return FPT_ERR_UNSUPPORTED;
   if (!(scale > 0.0f) || !(scale < 1e30f)) return FPT_ERR_BAD_ARG;

@@ -273,8 +273,8 @@ PyObject* kv_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
     c.need(Call::ld(k.t()) == Call::ld(v.t()));
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = c_kv_gather(c.stream, &cache, first, ends, (int)n_seqs, M, k.t().data_ptr(), v.t().data_ptr(), Call::ld(k.t()), ws.data_ptr(),
-                       (size_t)ws.numel());
+    code = c_kv_gather(c.stream, &cache, first, ends, (int)n_seqs, M, M ? k.t().data_ptr() : nullptr, M ? v.t().data_ptr() : nullptr,
+                       Call::ld(k.t()), ws.data_ptr(), (size_t)ws.numel());
     Py_END_ALLOW_THREADS
     c.done(code);
     return pair(k, v);
@@ -332,9 +332,10 @@ PyObject* attn_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Held o{c.result(a[10], false, q.size(0), q.size(1))}, lse{truth(a[9]) ? c.result(Py_None, true, q.size(0), n_q) : nullptr};
     int code;
     Py_BEGIN_ALLOW_THREADS
-    code = c_attn_prompt(c.stream, q.data_ptr(), Call::ld(q), (int)q.size(0), k.data_ptr(), Call::ld(k), v.data_ptr(), Call::ld(v), (int)k.size(0),
-                         n_q, n_kv, (int)hd, cu_q, cu_k, (int)n_seqs, causal, scale, o.t().data_ptr(), Call::ld(o.t()),
-                         lse.o ? static_cast<float*>(lse.t().data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel());
+    const bool keys = k.size(0) > 0;
+    code = c_attn_prompt(c.stream, q.data_ptr(), Call::ld(q), (int)q.size(0), keys ? k.data_ptr() : nullptr, Call::ld(k),
+                         keys ? v.data_ptr() : nullptr, Call::ld(v), (int)k.size(0), n_q, n_kv, (int)hd, cu_q, cu_k, (int)n_seqs, causal, scale,
+                         o.t().data_ptr(), Call::ld(o.t()), lse.o ? static_cast<float*>(lse.t().data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel());
     Py_END_ALLOW_THREADS
     c.done(code);
     return pair(o, lse);

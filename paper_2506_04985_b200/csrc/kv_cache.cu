@@ -441,7 +441,7 @@ extern "C" int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int
 
 extern "C" int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int32_t* first, const int32_t* cu_out, int n_seqs,
                              int M, void* K_out, void* V_out, int ld, void* workspace, size_t workspace_bytes) {
-  if (!cu_out || !K_out || !V_out || n_seqs <= 0 || M <= 0) return FPT_ERR_BAD_ARG;
+  if (!cu_out || n_seqs <= 0 || M < 0 || !K_out != (M == 0) || !V_out != (M == 0)) return FPT_ERR_BAD_ARG;
   const int rc = check_cache(cache, true);
   if (rc) return rc;
   if (ld < (int64_t)cache->n_kv * cache->head_dim) return FPT_ERR_BAD_ARG;

@@ -86,3 +86,36 @@ def test_a_page_table_that_grows_between_calls():
             with pytest.raises(B.FptError) as e:
                 call()
             assert e.value.code == B.ERR_BAD_ARG
+
+
+def test_read_back_of_nothing():
+    """Prefixes that are all empty, a single one among them; into tensors of the caller's; an offset beyond is recorded as ever."""
+    rng = np.random.default_rng(4)
+    cache, *_ = paged(rng, [0, 0, 5], 16, 2, 64)
+    for n in (1, 3):
+        ws = workspace()
+        K, V = B.fpt_kv_gather(cache, i32([0] * (n + 1)), 0, ws=ws)
+        assert K.shape == V.shape == (0, 128) and K.dtype == torch.bfloat16 and B.fpt_check_status(ws) == B.OK
+        wide = guarded_empty((4, 256), torch.bfloat16)
+        B.fpt_kv_gather(cache, i32([0] * (n + 1)), 0, K=wide[:0, :128], V=wide[:0, 128:], first=i32([3] * n), ws=ws)
+        assert B.fpt_check_status(ws) == B.OK
+        B.fpt_kv_gather(cache, i32([0] * n + [5]), 0, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,lens", [(128, 4, 2, [5, 0, 300]), (64, 5, 1, [1]), (64, 2, 2, [3] * 150), (128, 32, 8, [17] * 40)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_without_any_key(hd, n_q, n_kv, lens, causal):
+    rng = np.random.default_rng(5)
+    q = bf16(rng, sum(lens) + 2, n_q * hd)
+    q[0] = math.nan
+    out, ws = guarded_empty(q.shape, torch.bfloat16), workspace()
+    out.fill_(7.0)
+    none = torch.empty((0, n_kv * hd), dtype=torch.bfloat16, device=DEV)
+    _, lse = B.fpt_attn_prompt(q.to(DEV), none, none, n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32([0] * (len(lens) + 1)), causal=causal,
+                               want_lse=True, O=out, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    rows = sum(lens)
+    assert (bf16_host(out)[:rows] == 0).all() and (bf16_host(out)[rows:] == 7).all() and np.isneginf(host(lse)[:rows]).all()
+    B.fpt_attn_prompt(q.to(DEV), none, none, n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32([0] * len(lens) + [1]), O=out, ws=ws)
+    assert B.fpt_check_status(ws) == B.ERR_INDEX
