@@ -369,7 +369,8 @@ int fpt_decoder_attn_out(void* stream, const void* A, int M, int k_o,
  *
  * Lengths, offsets, positions and page numbers lie on the device and are not known to the host: one out of range
  * never leads outside a buffer; it is recorded beside the status word (fpt_check_status returns FPT_ERR_INDEX until
- * fpt_reset_status, FPT_ERR_TIMEOUT where a wait gave up too), and the results of the sequences it concerns are unspecified.
+ * fpt_reset_status, FPT_ERR_TIMEOUT where a wait gave up too), and the results of the sequences it concerns are unspecified,
+ * those of the whole call where offsets do not ascend.
  *
  * The four calls take a workspace of fpt_workspace_bytes(FPT_OP_ATTN, 1, 1, 1) bytes (any sizes), cleared once by
  * fpt_reset_status.  It may be the one that the linears use if it is large enough, and as there, calls that may run

@@ -243,7 +243,7 @@ __device__ __forceinline__ TaskOrder task_order(const PromptParams& P, int lane)
     int keys = -1;
     if (s < P.n_seqs) {
       const int q0 = __ldg(P.cu_q + s), q1 = __ldg(P.cu_q + s + 1), k0 = __ldg(P.cu_k + s), k1 = __ldg(P.cu_k + s + 1);
-      if (q0 < 0 || q1 < q0 || q1 > P.M_q || k0 < 0 || k1 < k0 || k1 > P.M_k) {
+      if (!rows_fit(q0, q1, P.M_q) || !rows_fit(k0, k1, P.M_k)) {
         record_bad_index(P.status, kBadOffset);
       } else {
         keys = k1 - k0;
@@ -344,7 +344,7 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
     ti.key0 = __ldg(P.cu_k + lo);
     const int end_k = __ldg(P.cu_k + lo + 1);
     ti.len_k = end_k - ti.key0;
-    if (ti.row0 < 0 || end_q < ti.row0 || end_q > P.M_q || ti.key0 < 0 || end_k < ti.key0 || end_k > P.M_k) {
+    if (!rows_fit(ti.row0, end_q, P.M_q) || !rows_fit(ti.key0, end_k, P.M_k)) {
       if (lane == 0) record_bad_index(P.status, kBadOffset);
       return false;
     }
@@ -828,6 +828,11 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (lane == 0) {
           mbar_arrive_expect_tx(answered, 16);
           ask_for_a_block(answer, answered);
+          // (while the answer comes)  Of many sequences the search looks only at those that it meets, and one whose offsets do not ascend may
+          // have no task to be met by: block s looks at sequence s (there are more blocks than sequences, and each is somebody's).
+          if (!SPLIT && P.n_seqs > 32 * kPrHeld && bid < P.n_seqs &&
+              !(rows_fit(__ldg(P.cu_q + bid), __ldg(P.cu_q + bid + 1), P.M_q) && rows_fit(__ldg(P.cu_k + bid), __ldg(P.cu_k + bid + 1), P.M_k)))
+            record_bad_index(P.status, kBadOffset);
         }
         if (!wait_long<true>(answered, asked & 1u, abort_flag, P.status, 8)) { ok = false; break; }
         ++asked;

@@ -119,3 +119,24 @@ def test_prompt_without_any_key(hd, n_q, n_kv, lens, causal):
     assert (bf16_host(out)[:rows] == 0).all() and (bf16_host(out)[rows:] == 7).all() and np.isneginf(host(lse)[:rows]).all()
     B.fpt_attn_prompt(q.to(DEV), none, none, n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32([0] * len(lens) + [1]), O=out, ws=ws)
     assert B.fpt_check_status(ws) == B.ERR_INDEX
+
+
+@pytest.mark.parametrize("n", [20, 100, 129, 200, 5000])
+@pytest.mark.parametrize("what", ["queries", "keys", "queries, far", "keys of no query"])
+def test_prompt_offsets_that_do_not_ascend_are_recorded(n, what):
+    """Wherever it stands, and whether or not a task of the spoilt sequence would be looked for."""
+    rng = np.random.default_rng(n)
+    hd, n_q, n_kv, lens = 64, 2, 1, [4] * n
+    q, k, v = (t.to(DEV) for t in prompt_case(rng, hd, n_q, n_kv, lens, lens, pad=0))
+    for at in (3, n // 2, n - 2):
+        a, b = offsets(lens), offsets(lens)
+        if what == "keys of no query":
+            a[at:] -= 4
+        off = b if what.startswith("keys") else a
+        off[at] = 0 if what.endswith("far") else off[at - 1] - 2
+        ws, out = workspace(), guarded_empty(q.shape, torch.bfloat16)
+        B.fpt_attn_prompt(q, k, v, n_q, n_kv, i32(a.tolist()), cu_k=i32(b.tolist()), O=out, ws=ws)
+        assert B.fpt_check_status(ws) == B.ERR_INDEX, at
+        ws = workspace()
+        B.fpt_attn_prompt(q, k, v, n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32(offsets(lens).tolist()), O=out, ws=ws)
+        assert B.fpt_check_status(ws) == B.OK
