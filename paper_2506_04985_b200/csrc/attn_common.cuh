@@ -71,40 +71,29 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatil
 // What a page's codes are multiplied with before rounding.
 __device__ __forceinline__ float inverse_scale(float s) { return s >= 1.17549435e-38f ? __fdiv_rn(1.0f, s) : 0.0f; }
 
-// The task of this CTA in a launch over the pages (or blocks of rows) that packed sequences touch (attn_rules.h).  All sequences are
-// looked at side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the look: one round of
-// loads, where a binary search would wait for one load after the other.  Offsets that do not ascend can give one task to several
-// sequences, each with rows below M: the lowest has it, and its thread alone says what it found, so that no first row of one meets the
-// rows of another.
+// The task of this CTA in a launch over the pages (or blocks of rows) that packed sequences touch (attn_rules.h); false: none.  All
+// sequences are looked at side by side, and what is asked of the found one (its first row, its rows, its entry of `extra`) comes with the
+// look: one round of loads, where a binary search would wait for one load after the other.  Offsets that do not ascend can give one task to
+// several sequences, each with rows below M: claims are counted, the first alone is stored, so that no first row of one meets the rows of
+// another, and a task with more than one is nobody's.  (Counted by the barrier instead, or stored once the lowest is known: the kernels
+// around it came out 10 % slower, 8190 tokens 45 us against 41.)
 struct FoundTask { int seq, place, row0, rows, extra; };
-__device__ __forceinline__ FoundTask find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int M, int block,
-                                               int id, FoundTask* found /* shared */, uint32_t* status) {
-  if (threadIdx.x == 0) found->seq = INT32_MAX;
+__device__ __forceinline__ bool find_task(const int32_t* __restrict__ cu, const int32_t* __restrict__ extra, int n_seqs, int M, int block,
+                                          int id, FoundTask* found /* shared */, uint32_t* status) {
+  __shared__ int claims;
+  if (threadIdx.x == 0) claims = 0;
   __syncthreads();
-  FoundTask mine = {INT32_MAX, 0, 0, 0, 0};
   for (int s = threadIdx.x; s < n_seqs; s += blockDim.x) {
     const int lo = __ldg(cu + s), hi = __ldg(cu + s + 1), e = extra ? __ldg(extra + s) : 0;
     if (!rows_fit(lo, hi, M)) {
       if (blockIdx.x == 0) record_bad_index(status, kBadOffset);
     } else {
       const int place = place_of_task(lo, hi, s, block, id);
-      if (place >= 0 && mine.seq == INT32_MAX) {
-        mine = FoundTask{s, place, lo, hi - lo, e};
-        atomicMin(&found->seq, s);
-      }
+      if (place >= 0 && atomicAdd(&claims, 1) == 0) *found = FoundTask{s, place, lo, hi - lo, e};
     }
   }
   __syncthreads();
-  const int winner = found->seq;
-  if (winner == INT32_MAX) return FoundTask{-1, 0, 0, 0, 0};
-  if (mine.seq == winner) {                          // (one thread)
-    found->place = mine.place;
-    found->row0 = mine.row0;
-    found->rows = mine.rows;
-    found->extra = mine.extra;
-  }
-  __syncthreads();
-  return *found;
+  return claims == 1;
 }
 
 int check_cache(const fpt_kv_cache* c, bool with_storage);

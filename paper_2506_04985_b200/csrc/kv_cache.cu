@@ -131,10 +131,9 @@ __global__ void __launch_bounds__(T, (N <= 2 ? 1024 : 512) / T) rope_append_kern
   pdl_launch_dependents();
 
   const int head = blockIdx.y % P.n_kv, tid = threadIdx.x;
-  const FoundTask task = P.cu ? find_task(P.cu, P.ctx, P.n_seqs, P.M, P.by_row ? 0 : P.page, blockIdx.x, &found, P.status)
-                              : FoundTask{(int)blockIdx.x, 0, (int)blockIdx.x, 1, __ldg(P.ctx + blockIdx.x)};
+  if (P.cu && !find_task(P.cu, P.ctx, P.n_seqs, P.M, P.by_row ? 0 : P.page, blockIdx.x, &found, P.status)) return;
+  const FoundTask task = P.cu ? found : FoundTask{(int)blockIdx.x, 0, (int)blockIdx.x, 1, __ldg(P.ctx + blockIdx.x)};
   const int s = task.seq, row0 = task.row0, n_new = task.rows, ctx = task.extra;
-  if (s < 0) return;
   if (ctx < 0 || ctx > P.n_pos - n_new) {       // a position without a rotation
     if (tid == 0 && n_new > 0) record_bad_index(P.status, kBadPosition);
     return;
@@ -313,9 +312,9 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams P) {
   __shared__ FoundTask found;
   pdl_wait();
   pdl_launch_dependents();
-  const FoundTask task = find_task(P.cu, P.first, P.n_seqs, P.M, P.page, blockIdx.x, &found, P.status);
+  if (!find_task(P.cu, P.first, P.n_seqs, P.M, P.page, blockIdx.x, &found, P.status)) return;
+  const FoundTask task = found;
   const int s = task.seq, place = task.place, row0 = task.row0, n_rows = task.rows, first = task.extra, tid = threadIdx.x;
-  if (s < 0) return;
   if (first < 0 || first > INT32_MAX - 1024 - n_rows) {
     if (tid == 0) record_bad_index(P.status, kBadOffset);
     return;

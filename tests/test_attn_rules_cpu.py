@@ -47,13 +47,10 @@ def test_offsets_that_do_not_ascend_are_refused_or_share_tasks():
 
 
 def test_one_thread_says_what_was_found():
-    """Several threads may claim a task (offsets that do not ascend).  What they share is written by an atomic minimum and, past it, by the
-    one thread whose sequence that is: five words stored by two threads could mix a first row with another's rows."""
+    """Several threads may claim a task (offsets that do not ascend).  Only the one whose claim is the first stores what it found: five words
+    stored by two threads could mix a first row with another's rows; and it is a task only where there was no second."""
     text = open(os.path.join(CSRC, "attn_common.cuh")).read()
-    body = text[text.index("FoundTask find_task("):]
+    body = text[text.index("bool find_task("):]
     body = body[:body.index("\n}\n")]
-    loop, after = body.split("atomicMin(&found->seq, s);")
-    assert not re.search(r"\*found\s*=", body) and re.findall(r"found->(\w+)\s*=[^=]", loop) == ["seq"]
-    assert re.search(r"if \(mine\.seq == winner\) \{[^}]*\}", after)
-    guarded = re.search(r"if \(mine\.seq == winner\) \{([^}]*)\}", after).group(1)
-    assert sorted(re.findall(r"found->(\w+)\s*=[^=]", guarded)) == sorted(re.findall(r"found->(\w+)\s*=[^=]", after)) == ["extra", "place", "row0", "rows"]
+    assert re.findall(r"[^;{}\n]*\*found\s*=", body) == ["      if (place >= 0 && atomicAdd(&claims, 1) == 0) *found ="]
+    assert "found->" not in body and re.search(r"claims = 0;\s*__syncthreads\(\);", body) and body.rstrip().endswith("__syncthreads();\n  return claims == 1;")
