@@ -174,10 +174,13 @@ def _native():
     if _calls is None:
         if not os.path.exists(CALLS_PATH):
             raise RuntimeError(f"{CALLS_PATH} is missing: build it with `python -m paper_2506_04985_b200.build`")
+        from .build import calls_abi
         L = lib()
         loader = importlib.machinery.ExtensionFileLoader("_calls", CALLS_PATH)
         m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_calls", CALLS_PATH, loader=loader))
         loader.exec_module(m)
+        if getattr(m, "abi", None) != calls_abi():
+            raise RuntimeError(f"{CALLS_PATH} was built for another torch or interpreter than {calls_abi()}: build it with `python -m paper_2506_04985_b200.build`")
         m.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
                  for f in ("fpt_rope_append", "fpt_kv_gather", "fpt_attn_decode", "fpt_attn_prompt")), FptError)
         m.set_allocator(_for_calls(_allocator))

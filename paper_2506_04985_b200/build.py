@@ -3,7 +3,8 @@
     python -m paper_2506_04985_b200.build [-v]
 
 The library is a plain `nvcc -shared` of csrc/*.cu (no torch headers), the extension a `g++ -shared` of csrc/calls.cpp
-against torch's headers and libraries; each is rebuilt when a source is newer than the binary.
+against torch's headers and libraries; each is rebuilt when a source is newer than the binary, the extension also when it was
+built for another torch or interpreter.
 """
 import glob
 import os
@@ -47,16 +48,29 @@ def _run(cmd, what, verbose):
         raise RuntimeError(f"{os.path.basename(cmd[0])} failed building " + what)
 
 
+def calls_abi():
+    """What the extension is bound to: the interpreter's and torch's versions, which it carries as a text."""
+    import torch
+    return f"python {sys.version_info[0]}.{sys.version_info[1]} torch {torch.__version__}"
+
+
+def _calls_fit():
+    if _older(CALLS, [CALLS_SRC, DEPS[-1]]):
+        return False
+    with open(CALLS, "rb") as f:
+        return calls_abi().encode() + b"\0" in f.read()
+
+
 def build_calls(verbose=False, force=False):
-    if not force and not _older(CALLS, [CALLS_SRC, DEPS[-1]]):
+    if not force and _calls_fit():
         return CALLS
     import sysconfig
     import torch
     top = os.path.dirname(torch.__file__)
     inc = [os.path.join(top, "include"), os.path.join(top, "include", "torch", "csrc", "api", "include"),
            sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc_path()))), "include")]
-    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared"] + [f for i in inc for f in ("-isystem", i)] +
-           [CALLS_SRC, "-o", CALLS, "-L" + os.path.join(top, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f'-DFPT_CALLS_ABI="{calls_abi()}"'] +
+           [f for i in inc for f in ("-isystem", i)] + [CALLS_SRC, "-o", CALLS, "-L" + os.path.join(top, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
     _run(cmd, CALLS, verbose)
     return CALLS
 
