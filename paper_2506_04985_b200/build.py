@@ -7,6 +7,7 @@ against torch's headers and libraries; each is rebuilt when a source is newer th
 built for another torch or interpreter.
 """
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -76,14 +77,14 @@ def build_calls(verbose=False, force=False):
 
 
 def build(verbose=False, force=False):
-    build_calls(verbose, force)
-    if not force and not needs_build():
-        return LIB
-    cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-o", LIB] + SRC
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    _run(cmd, LIB, verbose)
+    if force or needs_build():
+        cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+               "-Xcompiler", "-fPIC", "-shared", "-o", LIB] + SRC
+        if verbose:
+            cmd += ["-Xptxas", "-v"]
+        _run(cmd, LIB, verbose)
+    if importlib.util.find_spec("torch"):        # without torch there is nobody to marshal for: the C library alone
+        build_calls(verbose, force)
     return LIB
 
 

@@ -24,3 +24,13 @@ def test_the_extension_of_another_torch_is_not_loaded(monkeypatch):
     assert B._calls is None
     monkeypatch.undo()
     assert B._native().abi == build.calls_abi()
+
+
+def test_the_library_is_built_without_torch(monkeypatch, tmp_path):
+    """A caller of the C functions alone."""
+    import sys
+    calls = tmp_path / "_calls.so"
+    monkeypatch.setattr(build, "CALLS", str(calls))
+    monkeypatch.setitem(sys.modules, "torch", None)
+    assert build.build() == build.LIB
+    assert not calls.exists()
