@@ -32,10 +32,10 @@ def test_another_page_table_takes_effect():
 
 
 def test_other_storage_takes_effect():
-    c, other = a_cache(), a_cache(n_pages=40)
+    c, other = a_cache(), a_cache(n_pages=10)
     c.k, c.v, c.k_scale, c.v_scale = other.k, other.v, other.k_scale, other.v_scale
     s = struct(c)
-    assert s.n_pages == 40
+    assert s.n_pages == 10
     assert [s.k, s.v, s.k_scale, s.v_scale] == [t.data_ptr() for t in (other.k, other.v, other.k_scale, other.v_scale)]
 
 
