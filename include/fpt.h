@@ -430,7 +430,8 @@ int fpt_kv_gather(void* stream, const fpt_kv_cache* cache, const int32_t* first,
  *   z_t = scale * sum_d q_d k_td,  O = sum_t softmax(z)_t v_t,  lse = log sum_t exp(z_t),   t < kv_len[s]
  *   Q [n_seqs, ld_q] bf16 and O [n_seqs, ld_o] bf16: n_q heads, O must not overlap Q; lse [n_seqs, n_q] f32 or NULL
  *   kv_len [n_seqs] int32, the new token included; 0: O = 0, lse = -inf.
- * A key or value is code * scale; pages whose value scale is below 2^-80 count as zeros.  The sums are float32; the weights
+ * A key or value is code * scale; pages whose value scale is below 2^-80 count as zeros, and value scales stay below 2^20 (beyond, the
+ * weights of pages with such small values would drop out of the sum of weights).  The sums are float32; the weights
  * enter the second product in fp16, scaled so that the largest lies between 2^9 and 2^15, queries the first one in fp16 after division by
  * a power of two that brings the head's largest magnitude into [2^14, 2^15) (exact but for values below 2^-28 of that).  The long axis is split over the SMs by
  * the lengths of all sequences: the same call gives the same bits, another batch may round a sequence's sums otherwise.

@@ -23,7 +23,6 @@
 
 namespace fpt {
 
-constexpr int kDecTile = 64;                       // tokens of a tile
 constexpr int kDecWarps = 4;                       // consumer warps, 16 tokens of a tile each
 constexpr int kDecThreads = (kDecWarps + 1) * 32;
 constexpr float kDecLift = 9.0f;                   // log2 of the weight of a score at the reference ...
@@ -107,18 +106,6 @@ __device__ __forceinline__ uint32_t add_acq_rel(uint32_t* counter) {
   asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
   return old;
 }
-
-// `total` tiles in `ctas` ranges: the first `longer` of them have each + 1 tiles, the others `each` (at least 1).
-struct Ranges {
-  int each, longer;
-  __device__ __forceinline__ int first_of(int i) const { return i * each + min(i, longer); }
-  __device__ __forceinline__ int cta_of(int x) const {
-    const int edge = longer * (each + 1);
-    return x < edge ? x / (each + 1) : longer + (x - edge) / each;
-  }
-};
-
-__device__ __forceinline__ int tiles_of(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile : 1; }
 
 // Four elements, from d on, of the finished head h of a row.
 __device__ __forceinline__ void finish(__nv_bfloat16* O, float* lse, int hd, int h, int d, float4 o, float m, float sum) {

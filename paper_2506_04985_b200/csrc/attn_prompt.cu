@@ -33,7 +33,6 @@
 
 namespace fpt {
 
-constexpr int kPrTile = 128;               // query rows of a tile, keys of a tile
 constexpr int kPrThreads = 512;
 constexpr int kPrSoftRegs = 176, kPrEndRegs = 80, kPrAuxRegs = 80;
 static_assert(128 * (2 * kPrSoftRegs + kPrEndRegs + kPrAuxRegs) <= kPrThreads * 128, "the warpgroups' registers exceed the launch's");
@@ -192,38 +191,6 @@ __device__ __forceinline__ int block_of_answer(uint32_t answer) {
 }
 
 constexpr int kPrHeld = 4;
-constexpr int kPrPartTiles = 4, kPrParts = 32;       // a part's tiles at the least, a task's parts at the most
-constexpr int kPrSplitGain = 6;                        // tiles less to walk through for which keys are split
-
-// The tasks of one sequence with more tiles of keys than L, which are its last ones, in equal parts of at most L tiles.  L is a quarter more
-// than an SM's share of all tiles, at least kPrPartTiles, and as much more as it takes for the workspace to hold the parts' sums.
-// (32 heads of 128 and 8 of keys: 64 queries behind 4 000 keys 62 -> 29 us, 256 behind 30 000 409 -> 163; 16 behind
-// 100 000, 8 heads: 1 197 -> 71; one prompt of 5 400, 5 heads and one of keys, 83 -> 62; of 4 000, 4 heads, 60 -> 43.)
-struct Splitting {
-  int len_k, len_q, places, per_log2, causal;                // places: tasks a unit
-  __host__ __device__ int most() const { return (int)(((uint32_t)len_k + kPrTile - 1) / kPrTile); }
-  // all its tasks' tiles
-  __host__ __device__ uint32_t tiles() const {
-    const int64_t first = (int64_t)len_k - len_q + (1 << per_log2);           // keys that the first task sees
-    const int least = !causal ? most() : first <= 0 ? 0 : first >= len_k ? most() : (int)((first + kPrTile - 1) / kPrTile);
-    return (uint32_t)(((int64_t)places * (most() + least) + 1) / 2);
-  }
-  __host__ __device__ int split(int L) const {
-    if (most() <= L || places <= 0) return 0;
-    const int64_t seen = (int64_t)L * kPrTile - ((int64_t)len_k - len_q);     // rows from the first on whose keys are L tiles or fewer
-    const int64_t from = !causal || seen <= 0 ? 0 : seen >> per_log2;
-    return from < places ? places - (int)from : 1;
-  }
-  __host__ __device__ int parts(int L) const {
-    const int p = (most() + L - 1) / L;
-    return p < 1 ? 1 : p > kPrParts ? kPrParts : p;
-  }
-  __host__ __device__ static int first_length(uint32_t all, int sms) {
-    const int share = (int)fminf((float)all * (1.25f / (float)sms), 1e9f) + 1;       // (a division of 64 bits would take longer than the search)
-    return share > kPrPartTiles ? share : kPrPartTiles;
-  }
-};
-
 // Where the tasks of up to 128 sequences begin and how many they are: lane l knows it of sequences l, l + 32, ...  Up to 32 are
 // taken in the order of their lengths, longest walk first, so that what is left at the end of the launch is short; more as they come.
 struct TaskOrder { int first[kPrHeld], count[kPrHeld], q0[kPrHeld], len_q[kPrHeld], k0[kPrHeld], len_k[kPrHeld], split, parts, slot; };

@@ -4,7 +4,7 @@ import re
 
 import numpy as np
 
-from attn_rules import CSRC, rules
+from attn_rules import CSRC, rules, splitting
 
 
 def packed(rng, n, longest, before, behind):
@@ -54,3 +54,64 @@ def test_one_thread_says_what_was_found():
     body = body[:body.index("\n}\n")]
     assert re.findall(r"[^;{}\n]*\*found\s*=", body) == ["      if (place >= 0 && atomicAdd(&claims, 1) == 0) *found ="]
     assert "found->" not in body and re.search(r"claims = 0;\s*__syncthreads\(\);", body) and body.rstrip().endswith("__syncthreads();\n  return claims == 1;")
+
+
+def test_ranges_of_tiles_cover_the_line():
+    R, rng = rules(), np.random.default_rng(2)
+    for _ in range(100):
+        total = int(rng.integers(1, 5000))
+        ctas = min(int(rng.integers(1, 500)), total)
+        each, longer = total // ctas, total % ctas
+        first = [R.range_first(each, longer, i) for i in range(ctas + 1)]
+        assert first[0] == 0 and first[-1] == total and min(np.diff(first)) >= 1
+        for x in [0, total - 1, *(int(x) for x in rng.integers(0, total, 30))]:
+            c = R.range_of(each, longer, x)
+            assert first[c] <= x < first[c + 1]
+    assert [R.dec_tiles(n) for n in (-5, 0, 1, 64, 65, 2 ** 31 - 257)] == [1, 1, 1, 1, 2, 2 ** 25 - 4]
+
+
+def tiles_of_places(len_k, len_q, per, causal, tile):
+    ends = [min((p + 1) * per, len_q) for p in range(-(-len_q // per))]
+    return [-(-(min(max(e + len_k - len_q, 0), len_k) if causal else len_k) // tile) for e in ends]
+
+
+def test_splitting_takes_the_tasks_with_many_keys():
+    """Those, and only those, with more than L tiles, which are the last ones; in parts of at most L, as far as the most parts go."""
+    R, rng = rules(), np.random.default_rng(3)
+    tile, most_parts = R.part_limits(0), R.part_limits(2)
+    for _ in range(3000):
+        per_log2, causal = int(rng.integers(4, 9)), bool(rng.integers(0, 2))
+        len_q, len_k = (int(np.exp(rng.uniform(0, np.log(top)))) - 1 for top in (5000, 200000))
+        L = int(np.exp(rng.uniform(0, np.log(2000))))
+        tiles = tiles_of_places(len_k, len_q, 1 << per_log2, causal, tile)
+        s = splitting(len_k, len_q, per_log2, causal, L)
+        assert s.most == -(-len_k // tile) and s.split == sum(t > L for t in tiles), (len_k, len_q, per_log2, causal, L)
+        assert all(t > L for t in tiles[len(tiles) - s.split:])
+        assert 1 <= s.parts <= most_parts and (s.parts * L >= s.most or s.parts == most_parts)
+        # a whole number of tiles a part, none twice, none left out
+        for t in tiles[len(tiles) - s.split:]:
+            n = min(s.parts, max(t, 1))
+            cut = [t * i // n for i in range(n + 1)]
+            assert cut[0] == 0 and cut[-1] == t and min(np.diff(cut)) >= 1
+
+
+def test_parts_of_mixed_batches_have_room():
+    """The length is raised until the parts' sums fit the workspace, whatever the lengths beside one another; it ends; and few tasks of one
+    long sequence are split as far as they can be."""
+    R, rng = rules(), np.random.default_rng(4)
+    for _ in range(300):
+        n, units, per_log2, sms, room = int(rng.integers(1, 33)), int(rng.integers(1, 9)), int(rng.integers(4, 9)), 148, int(rng.choice([125, 244]))
+        seqs = [(int(np.exp(rng.uniform(0, np.log(300000)))), int(rng.integers(0, 200))) for _ in range(n)]
+        if sum(-(-q >> per_log2) if q else 0 for _, q in seqs) * units > sms:
+            continue
+        total = sum(splitting(k, q, per_log2, True, 1).tiles for k, q in seqs) * units
+        L = R.first_length(total, sms)
+        assert L >= R.part_limits(1)
+        for step in range(200):
+            slots = sum(s.split * s.parts for s in (splitting(k, q, per_log2, True, L) for k, q in seqs)) * units
+            if slots <= room:
+                break
+            L += max(1, L // 8)
+        assert slots <= room and step < 199
+    lone = splitting(100_000, 16, 6, True, R.first_length(782, 148))
+    assert (lone.split, lone.parts) == (1, 32)

@@ -140,3 +140,115 @@ def test_prompt_offsets_that_do_not_ascend_are_recorded(n, what):
         ws = workspace()
         B.fpt_attn_prompt(q, k, v, n_q, n_kv, i32(offsets(lens).tolist()), cu_k=i32(offsets(lens).tolist()), O=out, ws=ws)
         assert B.fpt_check_status(ws) == B.OK
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_infinities_keep_their_sign_and_nan_their_place(hd):
+    rng = np.random.default_rng(23)
+    n_q, n_kv, lens = 4, 2, [200, 70, 30]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, lens, lens, pad=0)
+    v[150, 3] = math.inf
+    v[190, 3] = -math.inf
+    v[20, 5] = -math.inf
+    v[199, hd + 1] = math.nan
+    k[180, hd:] = math.nan
+    v[260, :] = math.nan
+    k[205, 0] = math.inf
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32(offsets(lens).tolist()), want_lse=True)
+    check_prompt(o, lse, q, k, v, n_q, n_kv, hd, lens, lens, True)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_parts_keep_infinities_and_nan_apart(hd):
+    rng = np.random.default_rng(51)
+    n_q, n_kv, len_q, len_k = 4, 2, [100], [3000]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, len_q, len_k, pad=0)
+    v[2950, 3] = math.inf
+    v[2960, 4] = -math.inf
+    v[2990, 5] = math.nan
+    v[500, 7] = -math.inf
+    v[1000, hd + 2] = math.nan
+    k[2980, :hd] = math.nan
+    o, lse = B.fpt_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), n_q, n_kv, i32([0, 100]), cu_k=i32([0, 3000]), want_lse=True)
+    check_prompt(o, lse, q, k, v, n_q, n_kv, hd, len_q, len_k, True)
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,lens,pre", [
+    (128, 8, 2, [33, 200, 5], [0, 100, 700]), (64, 10, 2, [3, 9, 0, 4], [5, 5, 5, 5]), (64, 2, 1, [3] * 150, [7] * 150), (128, 4, 1, [16], [4000])])
+def test_prompt_that_begins_behind_the_first_row(hd, n_q, n_kv, lens, pre):
+    rng = np.random.default_rng(5)
+    len_k = [a + b for a, b in zip(lens, pre)]
+    q, k, v = prompt_case(rng, hd, n_q, n_kv, lens, len_k, pad=9)
+    at_q, at_k = 5, 7
+    Q, K, V = (torch.cat([torch.full((n, t.shape[1]), math.nan, dtype=t.dtype), t]) for t, n in ((q, at_q), (k, at_k), (v, at_k)))
+    out, ws = guarded_empty(Q.shape, torch.bfloat16), workspace()
+    out.fill_(7.0)
+    _, lse = B.fpt_attn_prompt(Q.to(DEV), K.to(DEV), V.to(DEV), n_q, n_kv, i32((offsets(lens) + at_q).tolist()),
+                               cu_k=i32((offsets(len_k) + at_k).tolist()), want_lse=True, O=out, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_prompt(out[at_q:], lse[at_q:], q, k, v, n_q, n_kv, hd, lens, len_k, True)
+    assert (bf16_host(out)[:at_q] == 7).all() and (bf16_host(out)[at_q + sum(lens):] == 7).all()
+
+
+@pytest.mark.parametrize("new,ctx", [([70, 1, 30], [5, 63, 40]), ([1, 0, 2, 1, 0], [63, 5, 64, 127, 9])])
+def test_append_and_read_back_that_begin_behind_the_first_row(new, ctx):
+    rng = np.random.default_rng(6)
+    hd, page, n_q, n_kv, at = 64, 64, 4, 2, 6
+    cache, pages, codes, scales = paged(rng, [a + b for a, b in zip(new, ctx)], page, n_kv, hd)
+    rows = sum(new)
+    x = bf16(rng, rows + at + 3, (n_q + 2 * n_kv) * hd)
+    tab, ws, cu = table(300, hd), workspace(), offsets(new) + at
+    Q = guarded_empty((rows + at + 3, n_q * hd), torch.bfloat16)
+    Q.fill_(7.0)
+    B.fpt_rope_append(x.to(DEV), n_q, cache, torch.from_numpy(tab).to(DEV), i32(ctx), cu_new=i32(cu.tolist()), Q=Q, ws=ws)
+    y = x.float().numpy().reshape(-1, n_q + 2 * n_kv, hd)
+    for i, (n, c) in enumerate(zip(new, ctx)):
+        if n:
+            qk = OA.rope(y[cu[i]:cu[i + 1], :n_q + n_kv], tab[c:c + n], hd, False)
+            assert np.array_equal(bf16_host(Q)[cu[i]:cu[i + 1]].reshape(n, n_q, hd), qk[:, :n_q])
+            OA.append(qk[:, n_q:], codes[0], scales[0], pages[i], c, page)
+            OA.append(y[cu[i]:cu[i + 1], n_q + n_kv:], codes[1], scales[1], pages[i], c, page)
+    assert (bf16_host(Q)[:at] == 7).all() and (bf16_host(Q)[at + rows:] == 7).all()
+    for got, want in zip((cache.k_scale, cache.v_scale, cache.k, cache.v), (*scales, *codes)):
+        assert np.array_equal(host(got), want)
+    ends = [a + b for a, b in zip(new, ctx)]
+    K, V = (guarded_empty((sum(ends) + at + 2, n_kv * hd), torch.bfloat16) for _ in "kv")
+    K.fill_(7.0), V.fill_(7.0)
+    co = offsets(ends) + at
+    B.fpt_kv_gather(cache, i32(co.tolist()), K.shape[0], K=K, V=V, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    for i, e in enumerate(ends):
+        for got, j in ((K, 0), (V, 1)):
+            want = torch.from_numpy(OA.read(codes[j], scales[j], pages[i], 0, e, page)).to(torch.bfloat16).float().numpy().reshape(e, -1)
+            assert np.array_equal(bf16_host(got)[co[i]:co[i + 1]], want)
+    assert (bf16_host(K)[:at] == 7).all() and (bf16_host(K)[-2:] == 7).all()
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv", [(128, 8, 2), (64, 32, 2)])
+def test_decode_value_scales_far_apart(hd, n_q, n_kv):
+    """Pages whose values lie 2^109 apart beside one another, those below 2^-80 that count as zeros, and a page of zeros: the sums of
+    weights do not feel the scales."""
+    rng = np.random.default_rng(6)
+    page, lens = 16, [500, 40, 70]
+    cache, pages, codes, scales, q = decode_case(rng, hd, page, n_q, n_kv, lens)
+    for p, at in enumerate(pages[0]):
+        if at >= 0:
+            scales[1][at] = 2.0 ** (30, -79, 0, -3)[p % 4]
+    zero = pages[1][0]
+    scales[1][zero], codes[1][zero] = 0, 0
+    scales[1][pages[1][1:3]] = 2.0 ** 30
+    scales[1][pages[2][:5]] = 2.0 ** -79
+    cache.v_scale.copy_(torch.from_numpy(scales[1])), cache.v.copy_(torch.from_numpy(codes[1]))
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True)
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, page, hd ** -0.5)
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,lens", [(64, 1, 1, [60000]), (128, 4, 1, [45000]), (64, 16, 1, [33000]), (128, 20, 1, [40000, 3])])
+def test_decode_one_row_over_every_cta(hd, n_q, n_kv, lens):
+    """A row in more parts than the join looks at in a step, or has room for weights of."""
+    rng = np.random.default_rng(7)
+    cache, pages, codes, scales, q = decode_case(rng, hd, 64, n_q, n_kv, lens)
+    ws = workspace()
+    o, lse = B.fpt_attn_decode(q.to(DEV), cache, i32(lens), want_lse=True, ws=ws)
+    assert B.fpt_check_status(ws) == B.OK
+    check_decode(o, lse, lens, pages, codes, scales, q, n_q, hd, 64, hd ** -0.5)
