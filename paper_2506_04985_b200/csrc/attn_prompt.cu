@@ -296,6 +296,10 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
     }
     if (lo < 0) return false;
   } else {
+    // The search looks only at the sequences that it meets, and one whose offsets do not ascend may have no task to be met by: block s
+    // looks at sequence s (there are more blocks than sequences, and each is somebody's).
+    const int s = min(bid, P.n_seqs - 1);
+    const int q0 = __ldg(P.cu_q + s), q1 = __ldg(P.cu_q + s + 1), k0 = __ldg(P.cu_k + s), k1 = __ldg(P.cu_k + s + 1);
     const int id = P.n_tasks - 1 - turn;
     int hi = P.n_seqs;
     while (hi - lo > 1) {
@@ -304,6 +308,7 @@ __device__ __forceinline__ bool find_prompt_task(const PromptParams& P, const Ta
       if (below) lo += (31 - __clz(below)) * step;
       hi = min(hi, lo + step);
     }
+    if (!rows_fit(q0, q1, P.M_q) || !rows_fit(k0, k1, P.M_k)) record_bad_index(P.status, kBadOffset);
     place = id - ((__ldg(P.cu_q + lo) >> per_log2) + lo);
     ti.row0 = __ldg(P.cu_q + lo);
     const int end_q = __ldg(P.cu_q + lo + 1);
@@ -795,11 +800,6 @@ attn_prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (lane == 0) {
           mbar_arrive_expect_tx(answered, 16);
           ask_for_a_block(answer, answered);
-          // (while the answer comes)  Of many sequences the search looks only at those that it meets, and one whose offsets do not ascend may
-          // have no task to be met by: block s looks at sequence s (there are more blocks than sequences, and each is somebody's).
-          if (!SPLIT && P.n_seqs > 32 * kPrHeld && bid < P.n_seqs &&
-              !(rows_fit(__ldg(P.cu_q + bid), __ldg(P.cu_q + bid + 1), P.M_q) && rows_fit(__ldg(P.cu_k + bid), __ldg(P.cu_k + bid + 1), P.M_k)))
-            record_bad_index(P.status, kBadOffset);
         }
         if (!wait_long<true>(answered, asked & 1u, abort_flag, P.status, 8)) { ok = false; break; }
         ++asked;
