@@ -412,6 +412,8 @@ typedef struct fpt_kv_cache {
  *        held codes clamp(rne(q * (s_old * inv)), -127, 127) where s > s_old
  *     so a page's scale grows with its tokens and never shrinks while it keeps one (tokens taken back by a smaller ctx
  *     keep their part in it).  A page that a call writes belongs to one sequence and stands once in its row of pages.
+ *     The scales come from the values alone: those of a calibration (a static grid, as fpt_qparams gives one to the linears) cannot
+ *     be set, since the first tokens of a page take no notice of what k_scale and v_scale hold.
  */
 int fpt_rope_append(void* stream, const void* QKV, int M, int ld, int n_q,
                     const float* rope, int n_pos, int rot_dim, int layout,
@@ -447,8 +449,10 @@ int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, const fpt_kv
  *   M_k = 0, with K and V NULL: no sequence has keys.
  * float32 scores and sums; the weights enter the second product in bf16, scaled so that a row's largest is at most 2^8: values below
  * 2^119 / len_k in magnitude overflow no sum.  Values of hidden keys, infinities and NaN among them, reach no result.
- * Where few query rows would leave SMs idle, keys are split over them by the sizes and the lengths of all sequences, and a
- * second launch joins the parts: the same call gives the same bits, another batch may round a sequence's sums otherwise.
+ * Where few query rows would leave SMs idle, keys are split over them and a second launch joins the parts.  Whether they are follows from
+ * M_q, M_k and n_seqs, as if all sequences were equally long and M_q were all rows (at most 32 sequences, no more tasks than SMs); how, from the
+ * lengths.  So one long walk beside ordinary prompts, more sequences, or rows far behind the last sequence leave it whole: a call of
+ * its own is then quicker.  The same call gives the same bits, another batch may round a sequence's sums otherwise.
  */
 int fpt_attn_prompt(void* stream, const void* Q, int ld_q, int M_q, const void* K, int ld_k, const void* V, int ld_v,
                     int M_k, int n_q, int n_kv, int head_dim, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,

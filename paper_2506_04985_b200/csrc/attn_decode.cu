@@ -810,7 +810,8 @@ extern "C" int fpt_attn_decode(void* stream, const void* Q, int ld_q, int n_q, c
   P.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = (cudaStream_t)stream;
   // Three CTAs an SM where registers and shared memory allow it: with two, and as much in flight, a tile in each takes its time
-  // (131071 tokens of 8 heads: 57 and 64 us, 64 ragged sequences: 136 and 161).
+  // (131071 tokens of 8 heads: 57 and 64 us, 64 ragged sequences: 136 and 161, replayed from a graph; one call after the other the latter take
+  // 139 to 153 with three).
   if (cache->head_dim == 128)
     return P.group <= 8 ? launch_decode<128, 1, 3, 3>(st, cache, P) : launch_decode<128, 2, 3, 2>(st, cache, P);
   return P.group <= 8 ? launch_decode<64, 1, 6, 3>(st, cache, P) : launch_decode<64, 2, 4, 3>(st, cache, P);

@@ -49,8 +49,8 @@ constexpr int kPrSplitGain = 6;                        // tiles less to walk thr
 
 // The tasks of one sequence with more tiles of keys than L, which are its last ones, in equal parts of at most L tiles.  L is a quarter more
 // than an SM's share of all tiles, at least kPrPartTiles, and as much more as it takes for the workspace to hold the parts' sums.
-// (32 heads of 128 and 8 of keys: 64 queries behind 4 000 keys 62 -> 29 us, 256 behind 30 000 409 -> 163; 16 behind
-// 100 000, 8 heads: 1 197 -> 71; one prompt of 5 400, 5 heads and one of keys, 83 -> 62; of 4 000, 4 heads, 60 -> 43.)
+// (32 heads of 128 and 8 of keys: 64 queries behind 4 000 keys 62 -> 30 us, 256 behind 30 000 409 -> 164; 16 behind
+// 100 000, 8 heads and one of keys: 1 197 -> 70; one prompt of 5 400, 5 heads and one of keys, 83 -> 60; of 4 000, 4 heads and one, 60 -> 42.)
 struct Splitting {
   int len_k, len_q, places, per_log2, causal;                // places: tasks a unit
   FPT_RULE int most() const { return (int)(((uint32_t)len_k + kPrTile - 1) / kPrTile); }
